@@ -9,6 +9,11 @@
  * frontier's feature rows (Sec. 4.2.1, the feature-copy stage, here a copy
  * inside HBM).  Vertex and edge IDs are type-specific (Sec. 4.1.4).
  *
+ * Beside the mini-batches: the dense operators that a vertex model runs on
+ * gathered rows (root-mean-square norm, matrix product with an epilogue,
+ * distillation from a teacher's top logits), forward and backward, at the end
+ * of this file.
+ *
  * Conventions shared by every call:
  *  - Pointers marked "device" are HIP device addresses on the current device;
  *    "host" pointers are read before the call returns.
@@ -43,12 +48,15 @@ typedef enum hg_status {
 } hg_status;
 
 /* Element type of a feature table.  The gather copies bytes; the type only
- * fixes the element size (4, 2, 2 bytes). */
+ * fixes the element size (4, 2, 2 bytes).  HG_DT_E4M3 (8 bits: 4 of exponent,
+ * 3 of mantissa, no infinities, largest value 448) is a type of the dense
+ * operators only, not of feature tables. */
 typedef enum hg_dtype {
   HG_DT_NONE = 0,
   HG_DT_F32 = 1,
   HG_DT_F16 = 2,
-  HG_DT_BF16 = 3
+  HG_DT_BF16 = 3,
+  HG_DT_E4M3 = 4
 } hg_dtype;
 
 /* One node type (Sec. 4.1.4: features are stored per node type, in an ID
@@ -561,6 +569,193 @@ hg_status hg_debug_philox(const uint32_t *ctr, uint64_t key, int64_t n,
 hg_status hg_bench_philox(uint64_t rng_seed, int32_t hop, int32_t etype, int64_t n_groups,
                           uint32_t lim, uint64_t *count, hipEvent_t start, hipEvent_t stop,
                           hipStream_t stream);
+
+/* ---- Dense operators on gathered rows -----------------------------------------
+ * What a vertex model computes from a mini-batch's feature rows.  Shared rules:
+ *  - Matrices are row-major with contiguous columns; a stride is the number of
+ *    elements between rows (any value >= 0 for an input, so that a broadcast
+ *    row has stride 0; at least the row's length for an output).  Rows need
+ *    the alignment of their element type only.
+ *  - Arrays are device memory on the current device, borrowed until the work
+ *    on `stream` is done.  Every call is asynchronous, allocates nothing and
+ *    waits for nothing, so it can be captured in a graph.
+ *  - Types: float32, float16 and bfloat16 (`dtype`), and 8 bits (HG_DT_E4M3)
+ *    where a call says so.  Sums, statistics and everything between the reads
+ *    and the result are held in 32 bits; a result is rounded once, to nearest
+ *    even, unless a call says otherwise.
+ *  - A result does not depend on timing: no sum is made by atomics.
+ *  - Zero rows are valid (nothing is done), and then arrays may be NULL.
+ *    HG_EINVAL: a NULL array, a bad type, size or stride.  HG_EUNSUPPORTED: a
+ *    size of 2^31 or more.
+ *  - Workspaces come from the caller, 16-byte aligned, of at least the bytes
+ *    that the call's _workspace function gives for the same arguments (0: NULL
+ *    is valid); their contents are not kept.  Calls that overlap need one each.
+ *  - An output may not overlap any other array of its call except as said. */
+
+/* Root-mean-square norm with the residual's addition.  For row i < rows:
+ *   h = x[i] + residual[i]  (x[ids[i]] with ids; no residual: h = x)
+ *   s = 1 / sqrt(mean_j h_j^2 + eps),  y_j = h_j s weight_j
+ * sum (NULL: not written) receives h in `dtype`; the norm is of the unrounded h.
+ * y in `dtype`; or in 8 bits with a scale per row (out_dtype HG_DT_E4M3):
+ *   scale_i = max(max_j |y_j| / 448, 2^-126),  y8_j = e4m3(y_j / scale_i)
+ * so that y8_j scale_i stands for y_j.  A NaN anywhere in a row makes the
+ * row's y (and its scale) NaN; an infinity makes NaN at its own place (and
+ * the scale NaN) and zeros elsewhere.
+ * An id outside [0, x_rows) makes the row NaN (sum, y, scale): nothing is read
+ * for it and nothing waits to report it.
+ * sum may be x (without ids) or residual, y may be x (without ids) or
+ * residual, each with the same stride. */
+typedef struct hg_norm_args {
+  int64_t rows, dim;          /* dim >= 1 */
+  int32_t dtype, out_dtype;   /* out_dtype: dtype or HG_DT_E4M3 */
+  int32_t weight_dtype;       /* HG_DT_F32 or dtype; HG_DT_NONE: no weight (1) */
+  float eps;                  /* >= 0 */
+  const void *x;
+  int64_t x_stride, x_rows;   /* x_rows: rows of x, read with ids only */
+  const int64_t *ids;         /* [rows] or NULL */
+  const void *residual;       /* [rows, dim] or NULL */
+  int64_t residual_stride;
+  const void *weight;         /* [dim] */
+  void *y;
+  int64_t y_stride;
+  float *scale;               /* [rows], with HG_DT_E4M3 */
+  void *sum;
+  int64_t sum_stride;
+} hg_norm_args;
+hg_status hg_rms_norm(const hg_norm_args *args, hipStream_t stream);
+
+/* The backward pass of hg_rms_norm, from the rows that were normalised (x: the
+ * forward call's sum, or its x with the same ids when it had no residual), the
+ * gradient dy of y and the gradient dsum of sum (NULL: none):
+ *   g = dy weight,  dx = s (g - h s^2 mean(g h)) + dsum,
+ *   dweight_j = sum_i dy_ij h_ij s_i
+ * dx is the gradient of both x and residual (row i belongs to x[ids[i]]); dx or
+ * dweight may be NULL (not computed).  An 8-bit y counts as unrounded.  dx may
+ * be dy or dsum or (without ids) x, with the same stride.  dweight is summed
+ * over the rows in a fixed order. */
+typedef struct hg_norm_grad_args {
+  int64_t rows, dim;
+  int32_t dtype, weight_dtype;
+  float eps;
+  const void *x;
+  int64_t x_stride, x_rows;
+  const int64_t *ids;
+  const void *weight;
+  const void *dy;
+  int64_t dy_stride;
+  const void *dsum;
+  int64_t dsum_stride;
+  void *dx;
+  int64_t dx_stride;
+  float *dweight;             /* [dim] float32; zeros when rows == 0 */
+  void *workspace;
+  int64_t workspace_bytes;
+} hg_norm_grad_args;
+hg_status hg_rms_norm_grad(const hg_norm_grad_args *args, hipStream_t stream);
+int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim);
+
+/* Matrix product with bias, activation and residual in one pass:
+ *   z = x w^T + bias,  y = act(z) + residual
+ * x [m, k], w [n, k] (one row per output), bias [n] or NULL, residual [m, n]
+ * or NULL, y [m, n]; pre (NULL: not written) receives z for the backward pass.
+ * k may be 0 (the product is then 0).
+ * dtype of x and w: float32, float16, bfloat16, with y, pre and residual in the
+ * same type; or HG_DT_E4M3 with a scale per row of x and of w,
+ *   z_ij = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,
+ * and y, pre and residual in out_dtype (float32, float16 or bfloat16).
+ * act: gelu is z / (1 + exp(-2 u)), u = sqrt(2/pi) (z + 0.044715 z^3) (its tanh
+ * form); silu is z / (1 + exp(-z)).
+ * y may be residual with the same stride. */
+#define HG_ACT_NONE 0
+#define HG_ACT_RELU 1
+#define HG_ACT_GELU 2
+#define HG_ACT_SILU 3
+typedef struct hg_linear_args {
+  int64_t m, k, n;
+  int32_t dtype, out_dtype;
+  int32_t bias_dtype;         /* HG_DT_F32, HG_DT_F16 or HG_DT_BF16 */
+  int32_t act;                /* HG_ACT_* */
+  const void *x;
+  int64_t x_stride;
+  const float *x_scale;       /* [m], with HG_DT_E4M3 */
+  const void *w;
+  int64_t w_stride;
+  const float *w_scale;       /* [n], with HG_DT_E4M3 */
+  const void *bias;
+  const void *residual;
+  int64_t residual_stride;
+  void *y;
+  int64_t y_stride;
+  void *pre;
+  int64_t pre_stride;
+  void *workspace;
+  int64_t workspace_bytes;
+} hg_linear_args;
+hg_status hg_linear(const hg_linear_args *args, hipStream_t stream);
+int64_t hg_linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);
+
+/* The backward pass of hg_linear (float32, float16 and bfloat16):
+ *   dz = dy act'(pre),  dx = dz w,  dw = dz^T x,  dbias_j = sum_i dz_ij
+ * pre: the forward call's (NULL with HG_ACT_NONE).  dx, dw (`dtype` or float32)
+ * and dbias (float32) may each be NULL (not computed).  The residual's
+ * gradient is dy.  relu's slope at 0 is 0.  With an activation, dz is rounded
+ * to `dtype` before the two products (dbias sums it unrounded). */
+typedef struct hg_linear_grad_args {
+  int64_t m, k, n;
+  int32_t dtype, dw_dtype, act;
+  const void *dy;
+  int64_t dy_stride;
+  const void *pre;
+  int64_t pre_stride;
+  const void *x;
+  int64_t x_stride;
+  const void *w;
+  int64_t w_stride;
+  void *dx;
+  int64_t dx_stride;
+  void *dw;
+  int64_t dw_stride;
+  float *dbias;
+  void *workspace;
+  int64_t workspace_bytes;
+} hg_linear_grad_args;
+hg_status hg_linear_grad(const hg_linear_grad_args *args, hipStream_t stream);
+int64_t hg_linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act);
+
+/* Distillation from a teacher's top logits.  Row i lists up to `top` classes
+ * with the teacher's logits; an entry with id -1 or a teacher logit of -inf is
+ * left out.  Over the entries that are left, and temperature T,
+ *   p = softmax(teacher_i / T),  q = softmax(logits_i / T) over all classes,
+ *   loss_i = sum_j p_j (log p_j - log q_{id_j})
+ *   grad_iv = row_weight_i / T (q_v - sum_{j: id_j = v} p_j)
+ * grad is the gradient of sum_i row_weight_i loss_i by the logits, in `dtype`;
+ * row_weight NULL: 1.  With the gradient of the losses as row_weight this is
+ * the backward pass; with loss and grad both given, one call does a training
+ * step's both directions.  loss or grad may be NULL (not computed).
+ * A row with no entry left has loss 0 and gradient 0, whatever its logits.  A
+ * row of weight 0 has gradient 0.  A class may be listed more than once.  A
+ * logit of -inf is a class of probability 0 (loss +inf where p > 0); rows
+ * with a NaN, an infinity of the other sign or only -inf logits, and rows with
+ * an id outside [-1, classes), have a NaN loss and gradient.
+ * grad may be logits with the same stride. */
+#define HG_MAX_TOP 1024
+typedef struct hg_distill_args {
+  int64_t rows, classes;      /* classes >= 1 */
+  int32_t top;                /* 0 .. HG_MAX_TOP (HG_EUNSUPPORTED past it) */
+  int32_t dtype, teacher_dtype;
+  float temperature;          /* > 0, finite */
+  const void *logits;         /* [rows, classes] */
+  int64_t logits_stride;
+  const int64_t *ids;         /* [rows, top] */
+  int64_t ids_stride;
+  const void *teacher;        /* [rows, top] */
+  int64_t teacher_stride;
+  const float *row_weight;    /* [rows] or NULL */
+  float *loss;                /* [rows] */
+  void *grad;                 /* [rows, classes] */
+  int64_t grad_stride;
+} hg_distill_args;
+hg_status hg_distill(const hg_distill_args *args, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -15,6 +15,9 @@ is not built; there is no CPU path.
     n_dst, src_gid = b.nodes(hop, ntype)
     indptr, src_local, dst_local, eid = b.edges(hop, etype)
     x = g.gather_features(b, ntype)
+
+The dense operators that a model runs on such rows (rms_norm, linear, distill and
+their backward passes) are in `dense`, and under this package's name.
 """
 from __future__ import annotations
 
@@ -51,7 +54,10 @@ ABI_SYMBOLS = ("hg_create", "hg_destroy", "hg_retire_stream", "hg_sample_blocks"
                "hg_pipeline_submit_layers", "hg_pipeline_submit_edges",
                "hg_blocks_free", "hg_last_error", "hg_debug_philox", "hg_bench_philox",
                "hg_sample_blocks_bundle_timed", "hg_pipeline_submit_timed", "hg_blocks_counts",
-               "hg_gather_rows_noalloc")
+               "hg_gather_rows_noalloc",
+               "hg_rms_norm", "hg_rms_norm_grad", "hg_rms_norm_grad_workspace",
+               "hg_linear", "hg_linear_workspace", "hg_linear_grad", "hg_linear_grad_workspace",
+               "hg_distill")
 
 HG_MAX_NEG = 64
 HG_MAX_TIMED_HOPS = 8
@@ -149,6 +155,14 @@ def _bind(lib: ctypes.CDLL) -> ctypes.CDLL:
         "hg_sample_layers_bundle": ([_P, _I32, _P, _P, _I32, _P, _P, _P, _I32, _P, _P], _I32),
         "hg_pipeline_submit_layers": ([_P, _I32, _P, _P, _I32, _P, _P], _I32),
         "hg_pipeline_submit_edges": ([_P, _I32, _P, _I32, _P, _P], _I32),
+        "hg_rms_norm": ([_P, _P], _I32),
+        "hg_rms_norm_grad": ([_P, _P], _I32),
+        "hg_rms_norm_grad_workspace": ([_I64, _I64], _I64),
+        "hg_linear": ([_P, _P], _I32),
+        "hg_linear_workspace": ([_I64, _I64, _I64, _I32], _I64),
+        "hg_linear_grad": ([_P, _P], _I32),
+        "hg_linear_grad_workspace": ([_I64, _I64, _I64, _I32, _I32], _I64),
+        "hg_distill": ([_P, _P], _I32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -923,3 +937,8 @@ def bench_philox(rng_seed: int, hop: int, etype: int, n_groups: int, lim: int,
                                           int(n_groups), int(lim) & 0xFFFFFFFF,
                                           count.data_ptr(), start, stop, _stream(stream)))
     return count
+
+
+from .dense import (HG_ACT_GELU, HG_ACT_NONE, HG_ACT_RELU, HG_ACT_SILU,  # noqa: E402,F401
+                    HG_DT_E4M3, HG_MAX_TOP, distill, linear, linear_grad, rms_norm,
+                    rms_norm_grad)
