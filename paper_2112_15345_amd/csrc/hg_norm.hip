@@ -12,33 +12,53 @@ namespace hg {
 namespace {
 
 constexpr int kBlock = 256;
+// Blocks of a walk over the rows: 8 on each of 256 compute units going forward; fewer
+// going backward, where each leaves a part of dweight.
+constexpr int64_t kResident = 2048;
+constexpr int64_t kParts = 1024;
 
-// Threads that share a row, and how to add over them.
+// Threads that share a row, and how to reduce over them.  Past a wavefront each
+// reduction goes through one of two LDS buffers in turn, so that one barrier is enough.
 template <int G>
 struct Group {
-  static constexpr int kRows = kBlock / G;  // rows of a block
-  float *red;                               // LDS, for G > 64
-  __device__ __forceinline__ float sum(float v) const {
-    v = lanes_sum<(G < 64 ? G : 64)>(v);
+  static constexpr int kRows = kBlock / G;  // rows of a block at a time
+  static constexpr int kLds = G > 64 ? 4 * (kBlock / 64) : 1;
+  float *red;  // LDS [kLds]
+  int turn = 0;
+  __device__ explicit Group(float *lds) : red(lds) {}
+  // Sums of two values.
+  __device__ __forceinline__ void sum(float &a, float &b) {
+    a = lanes_sum<(G < 64 ? G : 64)>(a);
+    b = lanes_sum<(G < 64 ? G : 64)>(b);
     if (G > 64) {
-      __syncthreads();  // red may hold an earlier reduction that is still read
-      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+      float *const r = red + (turn ^= 1) * 2 * (kBlock / 64);
+      if ((threadIdx.x & 63) == 0) {
+        r[threadIdx.x >> 6] = a;
+        r[kBlock / 64 + (threadIdx.x >> 6)] = b;
+      }
       __syncthreads();
-      v = 0.0f;
+      a = b = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kBlock / 64; ++i) v += red[i];
+      for (int i = 0; i < kBlock / 64; ++i) {
+        a += r[i];
+        b += r[kBlock / 64 + i];
+      }
     }
+  }
+  __device__ __forceinline__ float sum(float v) {
+    float none = 0.0f;
+    sum(v, none);
     return v;
   }
-  __device__ __forceinline__ uint32_t max(uint32_t v) const {
-    v = lanes_max<(G < 64 ? G : 64)>(v);
+  __device__ __forceinline__ uint32_t max(uint32_t v) {
+    v = lanes_max_bits<(G < 64 ? G : 64)>(v);
     if (G > 64) {
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = __uint_as_float(v);
+      float *const r = red + (turn ^= 1) * 2 * (kBlock / 64);
+      if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = __uint_as_float(v);
       __syncthreads();
       v = 0;
 #pragma unroll
-      for (int i = 0; i < kBlock / 64; ++i) v = ::max(v, __float_as_uint(red[i]));
+      for (int i = 0; i < kBlock / 64; ++i) v = ::max(v, __float_as_uint(r[i]));
     }
     return v;
   }
@@ -94,24 +114,35 @@ __device__ __forceinline__ void load_weight(const hg_norm_args &A, int64_t c, in
   }
 }
 
-// h of one vector of row i; bad: the id is out of range.
-template <typename T>
-__device__ __forceinline__ void load_h(const hg_norm_args &A, int64_t i, int64_t at, bool bad,
-                                       int64_t c, int n, float *h) {
-  constexpr int V = kVec<T>;
-  Vec<T> t;
-  if (bad) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = j < n ? __builtin_nanf("") : 0.0f;
-  } else {
-    t.load(static_cast<const T *>(A.x) + at * A.x_stride + c, n);
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = float(t.e[j]);
+// The row that position i stands for: its place in x, or -1 where the id is out of
+// range.
+struct Source {
+  const int64_t *ids;
+  int64_t rows;
+  __device__ __forceinline__ int64_t at(int64_t i) const {
+    if (!ids) return i;
+    const int64_t v = ids[i];
+    return v >= 0 && v < rows ? v : -1;
   }
-  if (A.residual) {
-    t.load(static_cast<const T *>(A.residual) + i * A.residual_stride + c, n);
+};
+
+template <typename T>
+__device__ __forceinline__ void fill_nan(Vec<T> &t) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) h[j] += float(t.e[j]);
+  for (int j = 0; j < kVec<T>; ++j) t.e[j] = T(__builtin_nanf(""));
+}
+
+// One vector (n > 0 elements of it) of a row of x; its elements past n are 0.
+template <typename T, Move M = Move::kStreamed>
+__device__ __forceinline__ void load_x(const void *x, int64_t stride, int64_t at, int c, int n,
+                                       Vec<T> &t) {
+  if (at >= 0) {
+    t.template load<M>(static_cast<const T *>(x) + at * stride + c, n);
+  } else {
+    fill_nan(t);
+#pragma unroll
+    for (int j = 0; j < kVec<T>; ++j)
+      if (j >= n) t.e[j] = T(0.0f);
   }
 }
 
@@ -120,136 +151,182 @@ __device__ __forceinline__ void store_row(T *p, const float *v, int n) {
   Vec<T> t;
 #pragma unroll
   for (int j = 0; j < kVec<T>; ++j) t.e[j] = T(v[j]);
-  t.store(p, n);
+  t.template store<Move::kStreamed>(p, n);
 }
 
-// NV vectors a lane hold the row; NV == 0: the row is read twice instead.
+// NV vectors a lane hold the row (NV > 0).  Groups walk over the rows and load the next
+// one while this one is reduced and written.
 template <typename T, int G, int NV, bool E4M3>
 __global__ __launch_bounds__(kBlock) void k_rms_norm(hg_norm_args A) {
   constexpr int V = kVec<T>;
-  __shared__ float red[kBlock / 64];
-  const Group<G> grp{red};
-  const int64_t i = int64_t(blockIdx.x) * Group<G>::kRows + threadIdx.x / G;
+  constexpr int kRows = Group<G>::kRows;
+  __shared__ float red[Group<G>::kLds];
+  Group<G> grp(red);
   const int lane = threadIdx.x % G;
-  if (i >= A.rows) return;  // whole groups: no block barrier follows for G <= 64, and kRows is 1 past it
   const int dim = int(A.dim);
-  const int64_t at = A.ids ? A.ids[i] : i;
-  const bool bad = A.ids && (at < 0 || at >= A.x_rows);
   const float inv = 1.0f / float(dim);
-  T *const y = static_cast<T *>(A.y) + i * A.y_stride;
-  uint8_t *const y8 = static_cast<uint8_t *>(A.y) + i * A.y_stride;
-  T *const sum = A.sum ? static_cast<T *>(A.sum) + i * A.sum_stride : nullptr;
-  if constexpr (NV > 0) {
+  const Source src{A.ids, A.x_rows};
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / G;
+  float w[NV][V];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * G + lane) * V;
+#pragma unroll
+    for (int j = 0; j < V; ++j) w[v][j] = 0.0f;
+    if (c < dim) load_weight<T>(A, c, dim - c, w[v]);
+  }
+  Vec<T> x[NV], r[NV];
+  auto load = [&](int64_t row, int64_t at) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * G + lane) * V;
+      if (c < dim) {
+        load_x<T>(A.x, A.x_stride, at, c, dim - c, x[v]);
+        if (A.residual)
+          r[v].template load<Move::kStreamed>(
+              static_cast<const T *>(A.residual) + row * A.residual_stride + c, dim - c);
+      }
+    }
+  };
+  int64_t next_at = i + step < A.rows ? src.at(i + step) : 0;
+  if (i < A.rows) load(i, src.at(i));
+  // (a group of 64 lanes or fewer leaves on its own; a larger one is the block)
+  for (; i < A.rows; i += step) {
+    T *const y = static_cast<T *>(A.y) + i * A.y_stride;
+    uint8_t *const y8 = static_cast<uint8_t *>(A.y) + i * A.y_stride;
     float h[NV][V];
     float ss = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * G + lane) * V;
-      const int n = dim - c;
-      if (n > 0) {
-        load_h<T>(A, i, at, bad, c, n, h[v]);
-        if (sum) store_row<T>(sum + c, h[v], n);
-      } else {
+      const bool in = (v * G + lane) * V < dim;
 #pragma unroll
-        for (int j = 0; j < V; ++j) h[v][j] = 0.0f;
+      for (int j = 0; j < V; ++j) {
+        h[v][j] = in ? float(x[v].e[j]) : 0.0f;
+        if (A.residual && in) h[v][j] += float(r[v].e[j]);
+        ss += h[v][j] * h[v][j];
       }
     }
+    if (i + step < A.rows) {
+      load(i + step, next_at);
+      next_at = i + 2 * step < A.rows ? src.at(i + 2 * step) : 0;
+    }
+    if (A.sum) {
+      T *const sum = static_cast<T *>(A.sum) + i * A.sum_stride;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < V; ++j) ss += h[v][j] * h[v][j];
+      for (int v = 0; v < NV; ++v) {
+        const int c = (v * G + lane) * V;
+        if (c < dim) store_row<T>(sum + c, h[v], dim - c);
+      }
+    }
     const float s = rsqrtf(grp.sum(ss) * inv + A.eps);
     uint32_t amax = 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * G + lane) * V;
-      const int n = dim - c;
-      if (n > 0) {
-        float w[V];
-        load_weight<T>(A, c, n, w);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          h[v][j] = h[v][j] * s * w[j];
-          if (E4M3 && j < n) amax = max(amax, mag(h[v][j]));
-        }
-        if (!E4M3) store_row<T>(y + c, h[v], n);
+      for (int j = 0; j < V; ++j) {
+        h[v][j] = h[v][j] * s * w[v][j];
+        if (E4M3 && c + j < dim) amax = max(amax, mag(h[v][j]));
       }
+      if (!E4M3 && c < dim) store_row<T>(y + c, h[v], dim - c);
     }
     if (E4M3) {
       const float sc = scale_of(grp.max(amax));
+      const float f = 1.0f / sc;
       if (lane == 0) A.scale[i] = sc;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int c = (v * G + lane) * V;
         if (c < dim) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) h[v][j] = h[v][j] / sc;
+          for (int j = 0; j < V; ++j) h[v][j] *= f;
           store_e4m3<V>(y8 + c, h[v], dim - c);
         }
       }
     }
-  } else {
-    float ss = 0.0f;
-    for (int c = lane * V; c < dim; c += G * V) {
-      float h[V];
-      load_h<T>(A, i, at, bad, c, dim - c, h);
-#pragma unroll
-      for (int j = 0; j < V; ++j) ss += h[j] * h[j];
-    }
-    const float s = rsqrtf(grp.sum(ss) * inv + A.eps);
-    float sc = 1.0f;
-    if (E4M3) {
-      uint32_t amax = 0;
-      for (int c = lane * V; c < dim; c += G * V) {
-        float h[V], w[V];
-        load_h<T>(A, i, at, bad, c, dim - c, h);
-        load_weight<T>(A, c, dim - c, w);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (j < dim - c) amax = max(amax, mag(h[j] * s * w[j]));
-      }
-      sc = scale_of(grp.max(amax));
-      if (lane == 0) A.scale[i] = sc;
-    }
-    // (a lane reads what it overwrites before it does, and no other lane's)
-    for (int c = lane * V; c < dim; c += G * V) {
-      const int n = dim - c;
-      float h[V], w[V];
-      load_h<T>(A, i, at, bad, c, n, h);
-      load_weight<T>(A, c, n, w);
-      if (sum) store_row<T>(sum + c, h, n);
-#pragma unroll
-      for (int j = 0; j < V; ++j) h[j] = E4M3 ? h[j] * s * w[j] / sc : h[j] * s * w[j];
-      if (E4M3)
-        store_e4m3<V>(y8 + c, h, n);
-      else
-        store_row<T>(y + c, h, n);
-    }
   }
 }
 
-// The backward pass.  Every group walks over rows and keeps its lanes' columns'
-// parts of dweight in registers; a block adds its groups' in LDS and writes one
-// part per block, which launch_sum_parts adds in order.
+// Rows that do not fit in a block's registers: a block reads its row twice (three
+// times for an 8-bit output).
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
+  constexpr int V = kVec<T>;
+  __shared__ float red[Group<kBlock>::kLds];
+  Group<kBlock> grp(red);
+  const int64_t i = blockIdx.x;
+  const int dim = int(A.dim);
+  const int64_t at = Source{A.ids, A.x_rows}.at(i);
+  auto load_h = [&](int c, float *h) {
+    Vec<T> t;
+    load_x<T, Move::kCached>(A.x, A.x_stride, at, c, dim - c, t);
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = float(t.e[j]);
+    if (A.residual) {
+      t.load(static_cast<const T *>(A.residual) + i * A.residual_stride + c, dim - c);
+#pragma unroll
+      for (int j = 0; j < V; ++j) h[j] += float(t.e[j]);
+    }
+  };
+  float ss = 0.0f;
+  for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+    float h[V];
+    load_h(c, h);
+#pragma unroll
+    for (int j = 0; j < V; ++j) ss += h[j] * h[j];
+  }
+  const float s = rsqrtf(grp.sum(ss) / float(dim) + A.eps);
+  float f = 1.0f;
+  if (E4M3) {
+    uint32_t amax = 0;
+    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      float h[V], w[V];
+      load_h(c, h);
+      load_weight<T>(A, c, dim - c, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < dim - c) amax = max(amax, mag(h[j] * s * w[j]));
+    }
+    const float sc = scale_of(grp.max(amax));
+    f = 1.0f / sc;
+    if (threadIdx.x == 0) A.scale[i] = sc;
+  }
+  // (a lane reads what it overwrites before it does, and no other lane's)
+  for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+    const int n = dim - c;
+    float h[V], w[V];
+    load_h(c, h);
+    load_weight<T>(A, c, n, w);
+    if (A.sum) store_row<T>(static_cast<T *>(A.sum) + i * A.sum_stride + c, h, n);
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = h[j] * s * w[j] * f;
+    if (E4M3)
+      store_e4m3<V>(static_cast<uint8_t *>(A.y) + i * A.y_stride + c, h, n);
+    else
+      store_row<T>(static_cast<T *>(A.y) + i * A.y_stride + c, h, n);
+  }
+}
+
+// The backward pass.  Groups walk over the rows as going forward, and keep their lanes'
+// columns' parts of dweight in registers; a block adds its groups' in LDS and writes one
+// part, which launch_sum_parts adds in order.  The two row sums are taken together.
 template <typename T, int G, int NV>
 __global__ __launch_bounds__(kBlock) void k_rms_norm_grad(hg_norm_grad_args A) {
   constexpr int V = kVec<T>;
   constexpr int kRows = Group<G>::kRows;
-  __shared__ float red[kBlock / 64];
+  __shared__ float red[Group<G>::kLds];
   __shared__ float wide[kRows > 1 ? kBlock * V : 1];
-  const Group<G> grp{red};
+  Group<G> grp(red);
   const int lane = threadIdx.x % G;
   const int dim = int(A.dim);
   const float inv = 1.0f / float(dim);
-  float *const part =
-      A.dweight ? static_cast<float *>(A.workspace) + int64_t(blockIdx.x) * dim : nullptr;
-  hg_norm_args N{};  // the forward's view of the rows and the weight
-  N.x = A.x;
-  N.x_stride = A.x_stride;
+  const Source src{A.ids, A.x_rows};
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  hg_norm_args N{};  // the forward's view of the weight
   N.weight = A.weight;
   N.weight_dtype = A.weight_dtype;
-  constexpr int NR = NV > 0 ? NV : 1;
-  float dw[NR][V], w[NR][V];
+  float dw[NV][V], w[NV][V];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = (v * G + lane) * V;
@@ -257,142 +334,181 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad(hg_norm_grad_args A) {
     for (int j = 0; j < V; ++j) dw[v][j] = w[v][j] = 0.0f;
     if (c < dim) load_weight<T>(N, c, dim - c, w[v]);
   }
-  if (NV == 0 && part)
-    for (int c = lane * V; c < dim; c += G * V)
-      for (int j = 0; j < V && c + j < dim; ++j) part[c + j] = 0.0f;
-  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / G; i < A.rows;
-       i += int64_t(gridDim.x) * kRows) {
-    const int64_t at = A.ids ? A.ids[i] : i;
-    const bool bad = A.ids && (at < 0 || at >= A.x_rows);
-    const T *const dy = static_cast<const T *>(A.dy) + i * A.dy_stride;
-    const T *const ds = A.dsum ? static_cast<const T *>(A.dsum) + i * A.dsum_stride : nullptr;
-    T *const dx = A.dx ? static_cast<T *>(A.dx) + i * A.dx_stride : nullptr;
-    float ss = 0.0f, gh = 0.0f;
-    if constexpr (NV > 0) {
-      float h[NV][V];
-      Vec<T> d[NV];
+  Vec<T> x[NV], d[NV];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * G + lane) * V;
-        const int n = dim - c;
-        if (n > 0) {
-          d[v].load(dy + c, n);
-          load_h<T>(N, i, at, bad, c, n, h[v]);
-        } else {
+  for (int v = 0; v < NV; ++v)
 #pragma unroll
-          for (int j = 0; j < V; ++j) h[v][j] = 0.0f, d[v].e[j] = T(0.0f);
-        }
-      }
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          ss += h[v][j] * h[v][j];
-          gh += float(d[v].e[j]) * w[v][j] * h[v][j];
-        }
-      const float s = rsqrtf(grp.sum(ss) * inv + A.eps);
-      const float k = grp.sum(gh) * inv * s * s;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * G + lane) * V;
-        const int n = dim - c;
-        if (n > 0) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) dw[v][j] += float(d[v].e[j]) * (h[v][j] * s);
-          if (dx) {
-            float o[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = s * (float(d[v].e[j]) * w[v][j] - h[v][j] * k);
-            if (ds) {
-              Vec<T> t;
-              t.load(ds + c, n);
-#pragma unroll
-              for (int j = 0; j < V; ++j) o[j] += float(t.e[j]);
-            }
-            store_row<T>(dx + c, o, n);
-          }
-        }
-      }
-    } else {
-      for (int c = lane * V; c < dim; c += G * V) {
-        float h[V], wt[V];
-        Vec<T> d;
-        d.load(dy + c, dim - c);
-        load_h<T>(N, i, at, bad, c, dim - c, h);
-        load_weight<T>(N, c, dim - c, wt);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          ss += h[j] * h[j];
-          gh += float(d.e[j]) * wt[j] * h[j];
-        }
-      }
-      const float s = rsqrtf(grp.sum(ss) * inv + A.eps);
-      const float k = grp.sum(gh) * inv * s * s;
-      for (int c = lane * V; c < dim; c += G * V) {
-        const int n = dim - c;
-        float h[V], wt[V], o[V];
-        Vec<T> d;
-        d.load(dy + c, n);
-        load_h<T>(N, i, at, bad, c, n, h);
-        load_weight<T>(N, c, n, wt);
-        if (part)
-          for (int j = 0; j < V && j < n; ++j) part[c + j] += float(d.e[j]) * (h[j] * s);
-        if (dx) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) o[j] = s * (float(d.e[j]) * wt[j] - h[j] * k);
-          if (ds) {
-            Vec<T> t;
-            t.load(ds + c, n);
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] += float(t.e[j]);
-          }
-          store_row<T>(dx + c, o, n);
-        }
-      }
-    }
-  }
-  if constexpr (NV > 0) {
-    if (!part) return;
+    for (int j = 0; j < V; ++j) x[v].e[j] = d[v].e[j] = T(0.0f);
+  auto load = [&](int64_t row, int64_t at) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * G + lane) * V;
-      if constexpr (kRows > 1) {
-        __syncthreads();
+      if (c < dim) {
+        load_x<T>(A.x, A.x_stride, at, c, dim - c, x[v]);
+        d[v].template load<Move::kStreamed>(static_cast<const T *>(A.dy) + row * A.dy_stride + c,
+                                            dim - c);
+      }
+    }
+  };
+  int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / G;
+  int64_t next_at = i + step < A.rows ? src.at(i + step) : 0;
+  if (i < A.rows) load(i, src.at(i));
+  for (; i < A.rows; i += step) {
+    Vec<T> ds[NV];
+    if (A.dsum && A.dx) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) wide[threadIdx.x * V + j] = dw[v][j];
-        __syncthreads();
-        if (threadIdx.x < G && c < dim) {
-          for (int r = 1; r < kRows; ++r)
+      for (int v = 0; v < NV; ++v) {
+        const int c = (v * G + lane) * V;
+        if (c < dim)
+          ds[v].template load<Move::kStreamed>(
+              static_cast<const T *>(A.dsum) + i * A.dsum_stride + c, dim - c);
+      }
+    }
+    float ss = 0.0f, gh = 0.0f;
+    Vec<T> xc[NV], dc[NV];
 #pragma unroll
-            for (int j = 0; j < V; ++j) dw[v][j] += wide[(r * G + lane) * V + j];
-          Vec<float, V> t;
+    for (int v = 0; v < NV; ++v) {
+      xc[v] = x[v];
+      dc[v] = d[v];
 #pragma unroll
-          for (int j = 0; j < V; ++j) t.e[j] = dw[v][j];
-          t.store(part + c, dim - c);
+      for (int j = 0; j < V; ++j) {
+        const float h = float(xc[v].e[j]);
+        ss += h * h;
+        gh += float(dc[v].e[j]) * w[v][j] * h;
+      }
+    }
+    if (i + step < A.rows) {
+      load(i + step, next_at);
+      next_at = i + 2 * step < A.rows ? src.at(i + 2 * step) : 0;
+    }
+    grp.sum(ss, gh);
+    const float s = rsqrtf(ss * inv + A.eps);
+    const float k = gh * inv * s * s;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * G + lane) * V;
+      float o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float h = float(xc[v].e[j]), dy = float(dc[v].e[j]);
+        dw[v][j] += dy * (h * s);
+        o[j] = s * (dy * w[v][j] - h * k);
+      }
+      if (A.dx && c < dim) {
+        if (A.dsum) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) o[j] += float(ds[v].e[j]);
         }
-      } else if (c < dim) {
-        Vec<float, V> t;
+        store_row<T>(static_cast<T *>(A.dx) + i * A.dx_stride + c, o, dim - c);
+      }
+    }
+  }
+  if (!A.dweight) return;
+  float *const part = static_cast<float *>(A.workspace) + int64_t(blockIdx.x) * dim;
 #pragma unroll
-        for (int j = 0; j < V; ++j) t.e[j] = dw[v][j];
-        t.store(part + c, dim - c);
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * G + lane) * V;
+    if constexpr (kRows > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < V; ++j) wide[threadIdx.x * V + j] = dw[v][j];
+      __syncthreads();
+      if (threadIdx.x < G) {
+        for (int r = 1; r < kRows; ++r)
+#pragma unroll
+          for (int j = 0; j < V; ++j) dw[v][j] += wide[(r * G + lane) * V + j];
+      }
+    }
+    if ((kRows == 1 || threadIdx.x < G) && c < dim) {
+      Vec<float, V> t;
+#pragma unroll
+      for (int j = 0; j < V; ++j) t.e[j] = dw[v][j];
+      t.store(part + c, dim - c);
+    }
+  }
+}
+
+// The same for rows that do not fit: read twice, dweight's part kept in the workspace.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args A) {
+  constexpr int V = kVec<T>;
+  __shared__ float red[Group<kBlock>::kLds];
+  Group<kBlock> grp(red);
+  const int dim = int(A.dim);
+  const Source src{A.ids, A.x_rows};
+  hg_norm_args N{};
+  N.weight = A.weight;
+  N.weight_dtype = A.weight_dtype;
+  float *const part =
+      A.dweight ? static_cast<float *>(A.workspace) + int64_t(blockIdx.x) * dim : nullptr;
+  if (part)
+    for (int c = threadIdx.x * V; c < dim; c += kBlock * V)
+      for (int j = 0; j < V && c + j < dim; ++j) part[c + j] = 0.0f;
+  for (int64_t i = blockIdx.x; i < A.rows; i += gridDim.x) {
+    const int64_t at = src.at(i);
+    const T *const dy = static_cast<const T *>(A.dy) + i * A.dy_stride;
+    float ss = 0.0f, gh = 0.0f;
+    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      float w[V];
+      Vec<T> d, x;
+      d.load(dy + c, dim - c);
+      load_x<T, Move::kCached>(A.x, A.x_stride, at, c, dim - c, x);
+      load_weight<T>(N, c, dim - c, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float h = float(x.e[j]);
+        ss += h * h;
+        gh += float(d.e[j]) * w[j] * h;
+      }
+    }
+    grp.sum(ss, gh);
+    const float inv = 1.0f / float(dim);
+    const float s = rsqrtf(ss * inv + A.eps);
+    const float k = gh * inv * s * s;
+    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      const int n = dim - c;
+      float w[V], o[V];
+      Vec<T> d, x;
+      d.load(dy + c, n);
+      load_x<T, Move::kCached>(A.x, A.x_stride, at, c, n, x);
+      load_weight<T>(N, c, n, w);
+      if (part)
+        for (int j = 0; j < V && j < n; ++j)
+          part[c + j] += float(d.e[j]) * (float(x.e[j]) * s);
+      if (A.dx) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = s * (float(d.e[j]) * w[j] - float(x.e[j]) * k);
+        if (A.dsum) {
+          Vec<T> t;
+          t.load(static_cast<const T *>(A.dsum) + i * A.dsum_stride + c, n);
+#pragma unroll
+          for (int j = 0; j < V; ++j) o[j] += float(t.e[j]);
+        }
+        store_row<T>(static_cast<T *>(A.dx) + i * A.dx_stride + c, o, n);
       }
     }
   }
 }
 
-// 64 columns a block: a wavefront reads 64 neighbours of a part, four take turns.
-__global__ __launch_bounds__(256) void k_sum_parts(const float *__restrict__ part, int64_t parts,
-                                                   int64_t n, float *__restrict__ out) {
-  __shared__ float red[256];
-  const int64_t j = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
+// 32 columns a block, 32 threads for each, which take turns over the parts and are
+// added in LDS: a thread then has few loads that follow each other (1024 parts, 128
+// columns: 4 us, where 4 threads for a column took 65).
+__global__ __launch_bounds__(1024) void k_sum_parts(const float *__restrict__ part, int64_t parts,
+                                                    int64_t n, float *__restrict__ out) {
+  __shared__ float red[32][33];
+  const int col = threadIdx.x & 31, turn = threadIdx.x >> 5;
+  const int64_t j = int64_t(blockIdx.x) * 32 + col;
   float s = 0.0f;
-  if (j < n)
-    for (int64_t p = threadIdx.x >> 6; p < parts; p += 4) s += part[p * n + j];
-  red[threadIdx.x] = s;
+  if (j < n) {
+#pragma unroll 8
+    for (int64_t p = turn; p < parts; p += 32) s += part[p * n + j];
+  }
+  red[turn][col] = s;
   __syncthreads();
-  if (threadIdx.x < 64 && j < n)
-    out[j] = red[threadIdx.x] + red[threadIdx.x + 64] + red[threadIdx.x + 128] +
-             red[threadIdx.x + 192];
+  // (a wavefront now has two columns: their 32 sums, added in a fixed tree)
+  const float v = lanes_sum<32>(red[threadIdx.x & 31][threadIdx.x >> 5]);
+  const int64_t o = int64_t(blockIdx.x) * 32 + (threadIdx.x >> 5);
+  if ((threadIdx.x & 31) == 0 && o < n) out[o] = v;
 }
 
 // How a row is shared: f.template run<G, NV>().
@@ -417,8 +533,14 @@ struct Forward {
   template <int G, int NV>
   hipError_t run() const {
     const int64_t blocks = ceil_div<int64_t>(A.rows, Group<G>::kRows);
-    hipLaunchKernelGGL((k_rms_norm<T, G, NV, E4M3>), dim3(unsigned(blocks)), dim3(kBlock), 0,
-                       stream, A);
+    if constexpr (NV == 0) {
+      hipLaunchKernelGGL((k_rms_norm_long<T, E4M3>), dim3(unsigned(blocks)), dim3(kBlock), 0,
+                         stream, A);
+    } else {
+      hipLaunchKernelGGL((k_rms_norm<T, G, NV, E4M3>),
+                         dim3(unsigned(blocks < kResident ? blocks : kResident)), dim3(kBlock), 0,
+                         stream, A);
+    }
     return hipGetLastError();
   }
 };
@@ -430,10 +552,14 @@ struct Backward {
   template <int G, int NV>
   hipError_t run() const {
     const int64_t blocks = ceil_div<int64_t>(A.rows, Group<G>::kRows);
-    const int64_t most = A.dweight ? rms_norm_grad_parts(A.rows, A.dim) : 2048;
+    const int64_t most = rms_norm_grad_parts(A.rows, A.dim);
     const int64_t grid = blocks < most ? blocks : most;
-    hipLaunchKernelGGL((k_rms_norm_grad<T, G, NV>), dim3(unsigned(grid)), dim3(kBlock), 0, stream,
-                       A);
+    if constexpr (NV == 0)
+      hipLaunchKernelGGL((k_rms_norm_grad_long<T>), dim3(unsigned(grid)), dim3(kBlock), 0, stream,
+                         A);
+    else
+      hipLaunchKernelGGL((k_rms_norm_grad<T, G, NV>), dim3(unsigned(grid)), dim3(kBlock), 0,
+                         stream, A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !A.dweight) return e;
     return launch_sum_parts(static_cast<const float *>(A.workspace), grid, A.dim, A.dweight,
@@ -452,7 +578,7 @@ hipError_t forward(const hg_norm_args &A, hipStream_t stream) {
 hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n, float *out,
                             hipStream_t stream) {
   if (n <= 0) return hipSuccess;
-  hipLaunchKernelGGL(k_sum_parts, dim3(unsigned(ceil_div<int64_t>(n, 64))), dim3(256), 0, stream,
+  hipLaunchKernelGGL(k_sum_parts, dim3(unsigned(ceil_div<int64_t>(n, 32))), dim3(1024), 0, stream,
                      part, parts, n, out);
   return hipGetLastError();
 }
@@ -460,7 +586,7 @@ hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n, float *
 // Parts of dweight: blocks of the backward pass, at most.
 int64_t rms_norm_grad_parts(int64_t rows, int64_t dim) {
   (void)dim;
-  return rows < 1024 ? rows : 1024;
+  return rows < kParts ? rows : kParts;
 }
 
 hipError_t launch_rms_norm(const hg_norm_args &A, hipStream_t stream) {
