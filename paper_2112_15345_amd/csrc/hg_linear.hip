@@ -50,39 +50,52 @@ __device__ __forceinline__ u32x4 widen(u32x2 v) {
   return o;
 }
 
-constexpr int kSlab = 128;       // bytes of a plain operand's row in a slab
+// A slab is 64 or 128 bytes (W) of a plain operand's row deep: 1 or 2 fragments (W / 64).
+// Elements of q in it:
+template <typename T, int W>
+constexpr int kDepth = W / int(sizeof(T));
 
-// Elements of q in a slab.
-template <typename T>
-constexpr int kDepth = kSlab / int(sizeof(T));
+// One step: 16 x 16 of C over a 16-byte fragment of each operand.  A lane holds, of row
+// (lane & 15), piece lane / 16 (for a slab's second fragment 4 more); which q a position
+// stands for does not matter as long as both operands agree.
+__device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, __bf16) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
+                                                 __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, _Float16) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, p),
+                                                __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, float) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[e]), __uint_as_float(q[e]), c, 0, 0,
+                                             0);
+  return c;
+}
 
-// One step: 16 x 16 of C over a slab, from two 16-byte fragments of each operand.
-// A lane holds, of row (lane & 15), the pieces lane / 16 and lane / 16 + 4 of the
-// slab; which q a position stands for does not matter as long as both operands
-// agree.
-__device__ __forceinline__ f32x4 mma(f32x4 c, const u32x4 (&p)[2], const u32x4 (&q)[2], __bf16) {
-#pragma unroll
-  for (int f = 0; f < 2; ++f)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p[f]),
-                                                __builtin_bit_cast(bf16x8, q[f]), c, 0, 0, 0);
-  return c;
-}
-__device__ __forceinline__ f32x4 mma(f32x4 c, const u32x4 (&p)[2], const u32x4 (&q)[2], _Float16) {
-#pragma unroll
-  for (int f = 0; f < 2; ++f)
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, p[f]),
-                                               __builtin_bit_cast(f16x8, q[f]), c, 0, 0, 0);
-  return c;
-}
-__device__ __forceinline__ f32x4 mma(f32x4 c, const u32x4 (&p)[2], const u32x4 (&q)[2], float) {
-#pragma unroll
-  for (int f = 0; f < 2; ++f)
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[f][e]), __uint_as_float(q[f][e]),
-                                               c, 0, 0, 0);
-  return c;
-}
+// A fragment as the matrix instructions take it.
+template <typename S>
+struct Step {
+  u32x4 v;
+  __device__ __forceinline__ Step() {}
+  __device__ __forceinline__ explicit Step(u32x4 f) : v(f) {}
+  __device__ __forceinline__ f32x4 mma(const Step &q, f32x4 c) const {
+    return hg::mma(c, v, q.v, S());
+  }
+};
+template <>
+struct Step<F8> {  // 16 elements: two steps of bfloat16
+  u32x4 v[2];
+  __device__ __forceinline__ Step() {}
+  __device__ __forceinline__ explicit Step(u32x4 f)
+      : v{widen(u32x2{f[0], f[1]}), widen(u32x2{f[2], f[3]})} {}
+  __device__ __forceinline__ f32x4 mma(const Step &q, f32x4 c) const {
+    c = hg::mma(c, v[0], q.v[0], __bf16());
+    return hg::mma(c, v[1], q.v[1], __bf16());
+  }
+};
+
 // ---- operands ------------------------------------------------------------------
 
 struct Operand {
@@ -94,17 +107,18 @@ struct Operand {
 // Where the 16-byte piece c of stored row r of an operand's slab lies in LDS
 // (B: extent of the tile along C's axis).  The pieces of a row are permuted by
 // the row so that the 64 lanes that read a fragment spread over all banks.
-template <typename S, bool Turned, int B>
+// T: the elements as they are in LDS.
+template <typename T, bool Turned, int B, int W>
 struct Slab {
-  typedef typename ComputeOf<S>::T T;
-  static constexpr int kRows = Turned ? kDepth<T> : B;           // stored rows
-  static constexpr int kRowBytes = Turned ? B * int(sizeof(T)) : kSlab;
+  static constexpr int kFrags = W / 64;
+  static constexpr int kRows = Turned ? kDepth<T, W> : B;        // stored rows
+  static constexpr int kRowBytes = Turned ? B * int(sizeof(T)) : W;
   static constexpr int kRowPieces = kRowBytes / 16;
   static constexpr int kBytes = kRows * kRowBytes;
   static constexpr int kTotal = kBytes / 16;
 
   __device__ static __forceinline__ int piece(int r, int c) {
-    if (!Turned) return r * kRowBytes + ((c ^ ((r >> 1) & 7)) << 4);
+    if (!Turned) return r * kRowBytes + ((c ^ (W == 128 ? (r >> 1) & 7 : (r >> 2) & 3)) << 4);
     if (sizeof(T) == 2) {
       // a fragment read takes 32 bytes of each of 16 rows (4 neighbours, 8 apart)
       const int f = kRowBytes >= 256 ? (r & 3) | (((r >> 3) & 1) << 2)
@@ -115,18 +129,19 @@ struct Slab {
     return r * kRowBytes + ((((c >> 2) ^ ((r >> 2) & 3)) << 2 | (c & 3)) << 4);
   }
 
-  // The two fragments of the 16 C-positions from `at` on.
-  __device__ static __forceinline__ void fragments(const char *lds, int at, u32x4 (&f)[2]) {
+  // The fragments of the 16 C-positions from `at` on.
+  __device__ static __forceinline__ void fragments(const char *lds, int at, u32x4 (&f)[kFrags]) {
     const int lane = threadIdx.x & 63;
     const int g = lane >> 4, x = lane & 15;
     if constexpr (!Turned) {
-      f[0] = *reinterpret_cast<const u32x4 *>(lds + piece(at + x, g));
-      f[1] = *reinterpret_cast<const u32x4 *>(lds + piece(at + x, g + 4));
+#pragma unroll
+      for (int h = 0; h < kFrags; ++h)
+        f[h] = *reinterpret_cast<const u32x4 *>(lds + piece(at + x, g + 4 * h));
     } else if constexpr (sizeof(T) == 2) {
       // position e of piece P is row 8 P + e; a transposing read gives a lane 4 rows of
       // its column from 4 x 16 elements that 16 lanes address 4 by 4
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < kFrags; ++h) {
         s16x4 v[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -141,7 +156,7 @@ struct Slab {
       }
     } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < kFrags; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * (g + 4 * h) + e;
@@ -151,33 +166,36 @@ struct Slab {
     }
   }
 
-  // The elements of piece `t` of the slab that starts at q0 (q < q_end): zeros outside.
-  __device__ static __forceinline__ u32x4 load(const Operand &O, int64_t c0, int64_t q0,
-                                               int64_t q_end, int t) {
-    constexpr int E = 16 / int(sizeof(T));  // elements of a piece
-    const int r = t / kRowPieces, c = t % kRowPieces;
-    const int64_t row = (Turned ? q0 : c0) + r;
-    const int64_t col = (Turned ? c0 : q0) + c * E;
-    const int64_t row_end = Turned ? q_end : O.rows, col_end = Turned ? O.rows : q_end;
-    S e[E];
-    __builtin_memset(e, 0, sizeof(e));
-    if (row < row_end && col < col_end) {
-      const S *p = static_cast<const S *>(O.p) + row * O.stride + col;
-      if (col + E <= col_end) {
-        __builtin_memcpy(e, p, sizeof(e));
-      } else {
-        const int n = int(col_end - col);
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (k < n) e[k] = p[k];
-      }
-    }
-    if constexpr (sizeof(S) == 1)
-      return widen(__builtin_bit_cast(u32x2, e));
-    else
-      return __builtin_bit_cast(u32x4, e);
-  }
 };
+
+// The elements of piece `t` of an operand's slab that starts at q0 (q < q_end), as they
+// go into LDS (L: its slab): zeros outside the operand.
+template <typename S, typename L, bool Turned>
+__device__ __forceinline__ u32x4 load_piece(const Operand &O, int64_t c0, int64_t q0,
+                                            int64_t q_end, int t) {
+  constexpr int E = 16 / int(sizeof(typename ComputeOf<S>::T));  // elements of a piece
+  const int r = t / L::kRowPieces, c = t % L::kRowPieces;
+  const int64_t row = (Turned ? q0 : c0) + r;
+  const int64_t col = (Turned ? c0 : q0) + c * E;
+  const int64_t row_end = Turned ? q_end : O.rows, col_end = Turned ? O.rows : q_end;
+  S e[E];
+  __builtin_memset(e, 0, sizeof(e));
+  if (row < row_end && col < col_end) {
+    const S *p = static_cast<const S *>(O.p) + row * O.stride + col;
+    if (col + E <= col_end) {
+      __builtin_memcpy(e, p, sizeof(e));
+    } else {
+      const int n = int(col_end - col);
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (k < n) e[k] = p[k];
+    }
+  }
+  if constexpr (sizeof(S) == 1)
+    return widen(__builtin_bit_cast(u32x2, e));
+  else
+    return __builtin_bit_cast(u32x4, e);
+}
 
 // ---- epilogue ------------------------------------------------------------------
 
@@ -196,25 +214,41 @@ struct Epilogue {
   float *part;  // [splits, rows, cols] sums to be joined, instead of the rest
 };
 
-__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + __expf(-v)); }
+// (a reciprocal within 1 unit of 2^-23, where a division would cost as much as the rest)
+__device__ __forceinline__ float sigmoid(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-v));
+}
 
-__device__ __forceinline__ float act_of(float z, int act) {
-  if (act == HG_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+template <int kAct>
+__device__ __forceinline__ float act_of(float z) {
+  if (kAct == HG_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+  if (kAct == HG_ACT_NONE) return z;
   // z sigmoid(v); an argument of -inf gives -0, not a NaN
-  if (act == HG_ACT_NONE) return z;
-  const float v = act == HG_ACT_SILU ? z : 1.5957691216057308f * (z + 0.044715f * z * z * z);
+  const float v = kAct == HG_ACT_SILU ? z : 1.5957691216057308f * (z + 0.044715f * z * z * z);
   return z == -INFINITY ? -0.0f : z * sigmoid(v);
 }
 
-__device__ __forceinline__ float act_slope(float z, int act) {
-  if (act == HG_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
-  if (act == HG_ACT_NONE) return 1.0f;
+template <int kAct>
+__device__ __forceinline__ float act_slope(float z) {
+  if (kAct == HG_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+  if (kAct == HG_ACT_NONE) return 1.0f;
   const float c = 1.5957691216057308f;
-  const float v = act == HG_ACT_SILU ? z : c * (z + 0.044715f * z * z * z);
-  const float dv = act == HG_ACT_SILU ? 1.0f : c * (1.0f + 0.134145f * z * z);
+  const float v = kAct == HG_ACT_SILU ? z : c * (z + 0.044715f * z * z * z);
+  const float dv = kAct == HG_ACT_SILU ? 1.0f : c * (1.0f + 0.134145f * z * z);
   const float s = sigmoid(v);
   const float rest = s * (1.0f - s);
   return rest == 0.0f ? s : s + z * rest * dv;  // (0 times an infinite dv far out)
+}
+
+// f(std::integral_constant of the activation): one branch outside a loop over values.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  if (act == HG_ACT_GELU)
+    f(std::integral_constant<int, HG_ACT_GELU>());
+  else if (act == HG_ACT_SILU)
+    f(std::integral_constant<int, HG_ACT_SILU>());
+  else if (act == HG_ACT_RELU)
+    f(std::integral_constant<int, HG_ACT_RELU>());
 }
 
 template <typename T, int N>
@@ -252,34 +286,65 @@ __device__ __forceinline__ void get_as(const void *base, int32_t dtype, int64_t 
     get<__bf16, N>(base, at, v, n);
 }
 
-// N neighbours v of row i from column j on, n of them in C.
-template <int N>
-__device__ __forceinline__ void finish(const Epilogue &E, int64_t i, int64_t j, int n, float *v) {
+// 8 columns of C, from j on, n of them in C: what is the same for every row.
+struct Columns {
+  int64_t j;
+  int n;
+  float bias[8], scale[8];
+  __device__ __forceinline__ Columns(const Epilogue &E, int64_t at) : j(at) {
+    n = int(max<int64_t>(0, min<int64_t>(8, E.cols - j)));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) bias[k] = 0.0f, scale[k] = 1.0f;
+    if (n > 0 && !E.part) {
+      if (E.bias) get_as<8>(E.bias, E.bias_dtype, j, bias, n);
+      if (E.col_scale) get<float, 8>(E.col_scale, j, scale, n);
+    }
+  }
+};
+
+// The columns' sums v of row i, to the result (n > 0; O: its type); `residual`: the row's.
+template <typename O, bool kPlain>
+__device__ __forceinline__ void finish(const Epilogue &E, const Columns &C, int64_t i,
+                                       const Vec<O, 8> &residual, float *v) {
+  if (kPlain) {
+    put<O, 8>(E.y, i * E.y_stride + C.j, v, C.n);
+    return;
+  }
   if (E.col_scale) {
     const float r = E.row_scale[i];
-    float s[N];
-    get<float, N>(E.col_scale, j, s, n);
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] *= r * s[k];
+    for (int k = 0; k < 8; ++k) v[k] *= r * C.scale[k];
   }
   if (E.bias) {
-    float b[N];
-    get_as<N>(E.bias, E.bias_dtype, j, b, n);
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += b[k];
+    for (int k = 0; k < 8; ++k) v[k] += C.bias[k];
   }
-  if (E.pre) put_as<N>(E.pre, E.dtype, i * E.pre_stride + j, v, n);
-  if (E.act != HG_ACT_NONE) {
+  if (E.pre) put<O, 8>(E.pre, i * E.pre_stride + C.j, v, C.n);
+  with_act(E.act, [&](auto act) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = act_of(v[k], E.act);
-  }
+    for (int k = 0; k < 8; ++k) v[k] = act_of<decltype(act)::value>(v[k]);
+  });
   if (E.residual) {
-    float r[N];
-    get_as<N>(E.residual, E.dtype, i * E.residual_stride + j, r, n);
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += r[k];
+    for (int k = 0; k < 8; ++k) v[k] += float(residual.e[k]);
   }
-  put_as<N>(E.y, E.dtype, i * E.y_stride + j, v, n);
+  put<O, 8>(E.y, i * E.y_stride + C.j, v, C.n);
+}
+template <typename O>
+__device__ __forceinline__ void load_residual(const Epilogue &E, const Columns &C, int64_t i,
+                                              Vec<O, 8> &r) {
+  if (E.residual)
+    r.template load<Move::kStreamed>(static_cast<const O *>(E.residual) + i * E.residual_stride + C.j, C.n);
+}
+// f(O()) with the result's type.
+template <typename F>
+__device__ __forceinline__ void with_type(int32_t dtype, F f) {
+  if (dtype == HG_DT_F32)
+    f(float());
+  else if (dtype == HG_DT_F16)
+    f(_Float16());
+  else
+    f(__bf16());
 }
 
 // ---- the tiled product ---------------------------------------------------------
@@ -292,20 +357,108 @@ struct Product {
   Epilogue E;
 };
 
+// Block b's tile.  Blocks go to the 8 XCDs in turn; each XCD is given a run of
+// neighbouring tiles, kGroup tiles high, so that the slabs that they share are read
+// through one L2.
+constexpr int kGroup = 8;
+__device__ __forceinline__ void tile_of(const Product &A, int64_t b, int64_t &ti, int64_t &tj) {
+  const int64_t n = int64_t(A.tiles_i) * A.tiles_j, even = n / kXcds * kXcds;
+  int64_t t = b < even ? xcd_block(b, even, true) : b;
+  const int64_t g = t / (int64_t(kGroup) * A.tiles_j);
+  const int64_t first = g * kGroup, high = min<int64_t>(kGroup, A.tiles_i - first);
+  t -= first * A.tiles_j;
+  ti = first + t % high;
+  tj = t / high;
+}
+
+// The waves' parts of C through LDS, 16 rows at a time: a lane's 4 neighbours in, 8
+// neighbours out, so that whole rows of the part are read and written together.  A lane
+// keeps its columns; the residual is loaded 16 rows ahead.
+// kPlain: nothing but the sums (the gradients).
+template <bool kPlain, int NI, int NJ>
+__device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i0, int64_t j0,
+                                          const f32x4 (&acc)[NI][NJ]) {
+  constexpr int WJ = NJ * 16;
+  constexpr int LD = WJ + 4;  // floats; the 4 spread the rows over the banks
+  constexpr int kAcross = WJ / 8, kDown = 64 / kAcross;  // lanes of a row, rows at a time
+  constexpr int U = 16 / kDown;
+  const Epilogue &E = A.E;
+  const int lane = threadIdx.x & 63;
+  float *const out = reinterpret_cast<float *>(lds) + (threadIdx.x >> 6) * 16 * LD;
+  const int r = lane / kAcross, c = lane % kAcross * 8;
+  const Columns C(E, j0 + c);
+  const auto exchange = [&](int a) {
+#pragma unroll
+    for (int b = 0; b < NJ; ++b)
+      *reinterpret_cast<f32x4 *>(out + (lane & 15) * LD + 16 * b + 4 * (lane >> 4)) = acc[a][b];
+    wave_sync();
+  };
+  const auto take = [&](int u, float *v) {
+    const float *const p = out + (u * kDown + r) * LD + c;
+    *reinterpret_cast<f32x4 *>(v) = *reinterpret_cast<const f32x4 *>(p);
+    *reinterpret_cast<f32x4 *>(v + 4) = *reinterpret_cast<const f32x4 *>(p + 4);
+  };
+  if (E.part) {
+#pragma unroll
+    for (int a = 0; a < NI; ++a) {
+      exchange(a);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + 16 * a + u * kDown + r;
+        float v[8];
+        take(u, v);
+        if (i < E.rows && C.n > 0)
+          put<float, 8>(E.part, (int64_t(blockIdx.y) * E.rows + i) * E.cols + C.j, v, C.n);
+      }
+      wave_sync();
+    }
+    return;
+  }
+  with_type(E.dtype, [&](auto type) {
+    typedef decltype(type) O;
+    Vec<O, 8> res[U];
+    const auto ahead = [&](int a) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + 16 * a + u * kDown + r;
+        if (!kPlain && i < E.rows && C.n > 0) load_residual<O>(E, C, i, res[u]);
+      }
+    };
+    ahead(0);
+#pragma unroll
+    for (int a = 0; a < NI; ++a) {
+      exchange(a);
+      Vec<O, 8> now[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) now[u] = res[u];
+      if (a + 1 < NI) ahead(a + 1);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + 16 * a + u * kDown + r;
+        float v[8];
+        take(u, v);
+        if (i < E.rows && C.n > 0) finish<O, kPlain>(E, C, i, now[u], v);
+      }
+      wave_sync();
+    }
+  });
+}
+
+// Any operands: slabs through registers.
 template <typename S, bool TP, bool TQ, int BI, int BJ>
 __global__ __launch_bounds__(256) void k_product(Product A) {
   typedef typename ComputeOf<S>::T T;
   constexpr int WI = BI / 2, WJ = BJ / 2;  // a wavefront's part: four, 2 x 2
   constexpr int NI = WI / 16, NJ = WJ / 16;
-  using SP = Slab<S, TP, BJ>;
-  using SQ = Slab<S, TQ, BI>;
+  using SP = Slab<T, TP, BJ, 128>;
+  using SQ = Slab<T, TQ, BI, 128>;
   constexpr int kStage = SP::kBytes + SQ::kBytes;
   constexpr int kOut = 4 * 16 * (WJ + 4) * 4;
   __shared__ __align__(16) char lds[kStage > kOut ? kStage : kOut];
   const int wave = threadIdx.x >> 6;
-  const int lane = threadIdx.x & 63;
-  const int64_t tile = blockIdx.x;
-  const int64_t j0 = (tile % A.tiles_j) * BJ, i0 = (tile / A.tiles_j) * BI;
+  int64_t ti, tj;
+  tile_of(A, blockIdx.x, ti, tj);
+  const int64_t i0 = ti * BI, j0 = tj * BJ;
   const int64_t q_begin = int64_t(blockIdx.y) * A.per_split;
   const int64_t q_end = min(A.depth, q_begin + A.per_split);
   const int wi = (wave >> 1) * WI, wj = (wave & 1) * WJ;
@@ -317,12 +470,14 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
     for (int b = 0; b < NJ; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   constexpr int LP = SP::kTotal / 256, LQ = SQ::kTotal / 256;
-  for (int64_t q = q_begin; q < q_end; q += kDepth<T>) {
+  for (int64_t q = q_begin; q < q_end; q += kDepth<T, 128>) {
     u32x4 vp[LP], vq[LQ];
 #pragma unroll
-    for (int u = 0; u < LP; ++u) vp[u] = SP::load(A.P, j0, q, q_end, u * 256 + threadIdx.x);
+    for (int u = 0; u < LP; ++u) 
+      vp[u] = load_piece<S, SP, TP>(A.P, j0, q, q_end, u * 256 + threadIdx.x);
 #pragma unroll
-    for (int u = 0; u < LQ; ++u) vq[u] = SQ::load(A.Q, i0, q, q_end, u * 256 + threadIdx.x);
+    for (int u = 0; u < LQ; ++u) 
+      vq[u] = load_piece<S, SQ, TQ>(A.Q, i0, q, q_end, u * 256 + threadIdx.x);
     __syncthreads();  // the last slab has been read
 #pragma unroll
     for (int u = 0; u < LP; ++u) {
@@ -342,40 +497,161 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
 #pragma unroll
     for (int a = 0; a < NI; ++a) SQ::fragments(lds + SP::kBytes, wi + 16 * a, fq[a]);
 #pragma unroll
-    for (int a = 0; a < NI; ++a)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int b = 0; b < NJ; ++b) acc[a][b] = mma(acc[a][b], fp[b], fq[a], T());
+      for (int a = 0; a < NI; ++a)
+#pragma unroll
+        for (int b = 0; b < NJ; ++b) acc[a][b] = mma(acc[a][b], fp[b][h], fq[a][h], T());
   }
-
-  // 16 rows at a time through LDS: a lane's 4 neighbours in, 8 neighbours out, so that
-  // whole rows of the part are read and written together
   __syncthreads();
-  constexpr int LD = WJ + 4;  // floats; the 4 spread the rows over the banks
-  float *const out = reinterpret_cast<float *>(lds) + wave * 16 * LD;
+  write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
+}
+
+// 16 bytes of zeros: where lanes past an operand's end load from.
+__device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
+
+// A wavefront's loads of an operand's slab straight into LDS: each moves 64 pieces to
+// 1024 bytes in a row, and a lane picks the piece that belongs where its 16 bytes go.
+template <typename S, bool Turned, int B, int W, int kWaves>
+struct Stream {
+  using L = Slab<S, Turned, B, W>;
+  static constexpr int E = 16 / int(sizeof(S));
+  static constexpr int kLoads = L::kBytes / 1024 / kWaves;
+  static_assert(L::kBytes % (1024 * kWaves) == 0, "whole loads for every wavefront");
+  const S *p[kLoads];
+  int r[kLoads], c[kLoads];  // the piece's stored row and its first element, in the slab
+  int64_t advance;
+
+  __device__ __forceinline__ void begin(const Operand &O, int64_t c0, int64_t q0) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    advance = Turned ? int64_t(kDepth<S, W>) * O.stride : kDepth<S, W>;
 #pragma unroll
-  for (int a = 0; a < NI; ++a) {
+    for (int u = 0; u < kLoads; ++u) {
+      const int t = (u * kWaves + wave) * 64 + lane;
+      r[u] = t / L::kRowPieces;
+      // (the permutation of a row's pieces is its own inverse)
+      c[u] = (L::piece(r[u], t % L::kRowPieces) - r[u] * L::kRowBytes) / 16 * E;
+      int64_t row = (Turned ? q0 : c0) + r[u], col = (Turned ? c0 : q0) + c[u];
+      // past the end along C: results there are not written, any row will do
+      if (Turned)
+        col = min<int64_t>(col, O.rows - E);
+      else
+        row = min<int64_t>(row, O.rows - 1);
+      p[u] = static_cast<const S *>(O.p) + row * O.stride + col;
+    }
+  }
+  // Starts the loads of the next slab, of which `left` of q are in the operand.
+  template <bool kWhole>
+  __device__ __forceinline__ void load(char *lds, int left) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int b = 0; b < NJ; ++b)
-      *reinterpret_cast<f32x4 *>(out + (lane & 15) * LD + 16 * b + 4 * (lane >> 4)) = acc[a][b];
-    wave_sync();
+    for (int u = 0; u < kLoads; ++u) {
+      const void *from = p[u];
+      if (!kWhole) from = (Turned ? r[u] : c[u]) < left ? from : g_zeros;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void *)from,
+          (__attribute__((address_space(3))) void *)(lds + (u * kWaves + wave) * 1024), 16, 0, 0);
+      p[u] += advance;
+    }
+  }
+};
+
+// Waits until at most n of this wavefront's loads are in flight.
+template <int n>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(n < 64, "the counter's range");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
+}
+
+// Aligned operands: a ring of kStages slabs in LDS, the loads of the next ones in
+// flight while one is multiplied.
+template <typename S, int BI, int BJ, int W, int kStages>
+constexpr int kRing = (BI + BJ) * W * kStages;  // bytes of LDS
+template <typename S, bool TP, bool TQ, int BI, int BJ, int kWavesI, int kWavesJ, int W,
+          int kStages>
+__global__ __launch_bounds__(64 * kWavesI *kWavesJ,
+                             (160 * 1024 / kRing<S, BI, BJ, W, kStages>) * kWavesI *kWavesJ / 4)  //
+    void k_product_direct(Product A) {
+  constexpr int kWaves = kWavesI * kWavesJ;
+  constexpr int WI = BI / kWavesI, WJ = BJ / kWavesJ;
+  constexpr int NI = WI / 16, NJ = WJ / 16;
+  using SP = Slab<S, TP, BJ, W>;
+  using SQ = Slab<S, TQ, BI, W>;
+  using LP = Stream<S, TP, BJ, W, kWaves>;
+  using LQ = Stream<S, TQ, BI, W, kWaves>;
+  constexpr int kFrags = W / 64;
+  constexpr int kStage = SP::kBytes + SQ::kBytes;
+  constexpr int kOut = kWaves * 16 * (WJ + 4) * 4;
+  static_assert(kOut <= kStages * kStage, "the parts of C fit where the slabs were");
+  __shared__ __align__(1024) char lds[kStages * kStage];
+  const int wave = threadIdx.x >> 6;
+  int64_t ti, tj;
+  tile_of(A, blockIdx.x, ti, tj);
+  const int64_t i0 = ti * BI, j0 = tj * BJ;
+  const int64_t q_begin = int64_t(blockIdx.y) * A.per_split;
+  const int64_t depth = min(A.depth - q_begin, A.per_split);
+  const int whole = int(depth / kDepth<S, W>), rest = int(depth % kDepth<S, W>);
+  const int slabs = whole + (rest > 0);
+  const int wi = wave / kWavesJ * WI, wj = wave % kWavesJ * WJ;
+
+  f32x4 acc[NI][NJ];
 #pragma unroll
-    for (int u = 0; u < 16 * WJ / 8 / 64; ++u) {
-      const int t = u * 64 + lane;
-      const int r = t / (WJ / 8), c = t % (WJ / 8) * 8;
-      const int64_t i = i0 + wi + 16 * a + r, j = j0 + wj + c;
-      if (i < A.E.rows && j < A.E.cols) {
-        float v[8];
-        *reinterpret_cast<f32x4 *>(v) = *reinterpret_cast<const f32x4 *>(out + r * LD + c);
-        *reinterpret_cast<f32x4 *>(v + 4) = *reinterpret_cast<const f32x4 *>(out + r * LD + c + 4);
-        const int n = int(min<int64_t>(8, A.E.cols - j));
-        if (A.E.part)
-          put<float, 8>(A.E.part, (int64_t(blockIdx.y) * A.E.rows + i) * A.E.cols + j, v, n);
-        else
-          finish<8>(A.E, i, j, n, v);
+  for (int a = 0; a < NI; ++a)
+#pragma unroll
+    for (int b = 0; b < NJ; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  LP lp;
+  LQ lq;
+  lp.begin(A.P, j0, q_begin);
+  lq.begin(A.Q, i0, q_begin);
+  const auto load = [&](int slab, char *to) {
+    if (slab < whole) {
+      lp.template load<true>(to, 0);
+      lq.template load<true>(to + SP::kBytes, 0);
+    } else if (slab < slabs) {
+      lp.template load<false>(to, rest);
+      lq.template load<false>(to + SP::kBytes, rest);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < kStages - 1; ++u) load(u, lds + u * kStage);
+  int now = 0, ahead = kStages - 1;  // places in the ring
+  const bool idle = i0 + wi >= A.E.rows || j0 + wj >= A.E.cols;  // no part of C for this wavefront
+  for (int slab = 0; slab < slabs; ++slab) {
+    // this wavefront's loads of the slab have landed (those of later ones may be in flight)
+    if (slab + kStages - 1 <= slabs)
+      wait_loads<(kStages - 2) * (LP::kLoads + LQ::kLoads)>();
+    else
+      wait_loads<0>();
+    // now everyone's have, and the slab that the next loads overwrite has been read
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    load(slab + kStages - 1, lds + ahead * kStage);
+    const char *const at = lds + now * kStage;
+    ahead = now;
+    now = now + 1 == kStages ? 0 : now + 1;
+    if (idle) continue;
+    u32x4 fp[NJ][kFrags], fq[NI][kFrags];
+#pragma unroll
+    for (int b = 0; b < NJ; ++b) SP::fragments(at, wj + 16 * b, fp[b]);
+#pragma unroll
+    for (int a = 0; a < NI; ++a) SQ::fragments(at + SP::kBytes, wi + 16 * a, fq[a]);
+#pragma unroll
+    for (int h = 0; h < kFrags; ++h) {
+      Step<S> tp[NJ];
+#pragma unroll
+      for (int b = 0; b < NJ; ++b) tp[b] = Step<S>(fp[b][h]);
+#pragma unroll
+      for (int a = 0; a < NI; ++a) {
+        const Step<S> tq(fq[a][h]);
+#pragma unroll
+        for (int b = 0; b < NJ; ++b) acc[a][b] = tp[b].mma(tq, acc[a][b]);
       }
     }
-    wave_sync();
   }
+  __syncthreads();
+  write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
 }
 
 // Adds the parts of a product in order, then the epilogue.
@@ -384,20 +660,26 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
   const int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (t >= E.rows * per_row) return;
   const int64_t i = t / per_row, j = t % per_row * 8;
-  const int n = int(min<int64_t>(8, E.cols - j));
+  float *const part = E.part;
+  E.part = nullptr;
+  const Columns C(E, j);
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int s = 0; s < splits; ++s) {
     float a[8];
-    get<float, 8>(E.part, (s * E.rows + i) * E.cols + j, a, n);
+    get<float, 8>(part, (s * E.rows + i) * E.cols + j, a, C.n);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += a[k];
   }
-  finish<8>(E, i, j, n, v);
+  with_type(E.dtype, [&](auto type) {
+    Vec<decltype(type), 8> r;
+    load_residual(E, C, i, r);
+    finish<decltype(type), false>(E, C, i, r, v);
+  });
 }
 
 // ---- dz and its column sums ------------------------------------------------------
 
-constexpr int kSumRows = 256;  // rows of C that one part of the column sums covers
+constexpr int kSumRows = 64;  // rows of C that one part of the column sums covers
 
 // dz = dy act'(pre) in T (dz NULL: not written), and the sums over the block's rows.
 // A wavefront takes 64 vectors of 8 columns; the block's four take turns over the rows.
@@ -413,19 +695,33 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, cons
   const int64_t r0 = chunk * kSumRows, r1 = min(m, r0 + kSumRows);
   const int left = int(min<int64_t>(8, n - j));
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  constexpr int U = 4;  // rows in flight
   if (left > 0)
-    for (int64_t i = r0 + wave; i < r1; i += 4) {
-      float v[8];
-      get<T, 8>(dy, i * dy_stride + j, v, left);
-      if (pre) {
-        float z[8];
-        get<T, 8>(pre, i * pre_stride + j, z, left);
+    for (int64_t i0 = r0 + wave; i0 < r1; i0 += 4 * U) {
+      Vec<T, 8> d[U], z[U];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= act_slope(z[k], act);
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + 4 * u;
+        if (i < r1) {
+          d[u].template load<Move::kStreamed>(dy + i * dy_stride + j, left);
+          if (pre) z[u].template load<Move::kStreamed>(pre + i * pre_stride + j, left);
+        }
       }
-      if (dz) put<T, 8>(dz, i * n + j, v, left);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] += v[k];
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + 4 * u;
+        if (i >= r1) break;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = float(d[u].e[k]);
+        with_act(act, [&](auto a) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] *= act_slope<decltype(a)::value>(float(z[u].e[k]));
+        });
+        if (dz) put<T, 8>(dz, i * n + j, v, left);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += v[k];
+      }
     }
   if (!part) return;
 #pragma unroll
@@ -446,7 +742,7 @@ int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
 int64_t size_of(int32_t dtype) {
   return dtype == HG_DT_F32 ? 4 : (dtype == HG_DT_E4M3 ? 1 : 2);
 }
-int64_t depth_of(int32_t dtype) { return kSlab / (dtype == HG_DT_F32 ? 4 : 2); }
+int64_t depth_of(int32_t dtype) { return 128 / (dtype == HG_DT_F32 ? 4 : 2); }
 
 // Into how many parts the depth is cut: enough for two blocks on each of 256 compute
 // units, each of at least 8 slabs.
@@ -459,6 +755,14 @@ int64_t splits_of(int64_t tiles, int64_t depth, int64_t slab) {
 int64_t splits_for(int64_t rows, int64_t cols, int64_t depth, int64_t slab) {
   if (rows <= 0 || cols <= 0) return 1;
   return splits_of(ceil_div<int64_t>(rows, kTile) * ceil_div<int64_t>(cols, kTile), depth, slab);
+}
+
+// Whether every 16-byte piece of an operand is aligned, and lies in it or outside it.
+template <typename S>
+bool is_direct(const Operand &O, bool turned, int64_t depth) {
+  constexpr int64_t E = 16 / int64_t(sizeof(S));
+  return reinterpret_cast<uintptr_t>(O.p) % 16 == 0 && O.stride % E == 0 &&
+         (turned ? O.rows : depth) % E == 0;
 }
 
 template <typename S, bool TP, bool TQ>
@@ -474,14 +778,32 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
   if (ti * tj >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
   A.tiles_i = int32_t(ti);
   A.tiles_j = int32_t(tj);
-  const int64_t slab = kDepth<typename ComputeOf<S>::T>;
+  const int64_t slab = kDepth<typename ComputeOf<S>::T, 128>;
   int64_t splits = parts ? splits_for(E.rows, E.cols, depth, slab) : 1;
   A.per_split = ceil_div<int64_t>(ceil_div<int64_t>(depth, slab), splits) * slab;
   if (A.per_split < slab) A.per_split = slab;
   splits = depth > 0 ? ceil_div<int64_t>(depth, A.per_split) : 1;
   if (splits > 1) A.E.part = parts;
-  hipLaunchKernelGGL((k_product<S, TP, TQ, kTile, kTile>), dim3(unsigned(ti * tj), unsigned(splits)),
-                     dim3(256), 0, stream, A);
+  const dim3 grid(unsigned(ti * tj), unsigned(splits));
+  const bool direct = is_direct<S>(P, TP, depth) && is_direct<S>(Q, TQ, depth);
+#ifndef HG_TI
+#define HG_TI 128
+#define HG_TJ 128
+#define HG_WI 2
+#define HG_WJ 2
+#define HG_W 128
+#define HG_ST 2
+#endif
+  {
+    if (direct) {
+      A.tiles_i = int32_t(ceil_div<int64_t>(E.rows, HG_TI));
+      A.tiles_j = int32_t(ceil_div<int64_t>(E.cols, HG_TJ));
+      hipLaunchKernelGGL((k_product_direct<S, TP, TQ, HG_TI, HG_TJ, HG_WI, HG_WJ, HG_W, HG_ST>), dim3(unsigned(A.tiles_i)*unsigned(A.tiles_j), unsigned(splits)), dim3(HG_WI*HG_WJ*64), 0,
+                         stream, A);
+    }
+  }
+  if (!direct)
+    hipLaunchKernelGGL((k_product<S, TP, TQ, kTile, kTile>), grid, dim3(256), 0, stream, A);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
   const int64_t threads = E.rows * ceil_div<int64_t>(E.cols, 8);
