@@ -63,10 +63,13 @@ struct Vec {
   template <Move M = Move::kCached>
   __device__ __forceinline__ void load(const T *p, int n, T rest = T(0.0f)) {
     if (n >= V) {
-      if constexpr (M == Move::kStreamed && sizeof(e) == 16) {
+      if constexpr (M == Move::kStreamed && sizeof(e) % 16 == 0) {
         typedef unsigned int W __attribute__((ext_vector_type(4), aligned(2)));
-        const W w = __builtin_nontemporal_load(as<const W>(p));
-        __builtin_memcpy(e, &w, sizeof(e));
+#pragma unroll
+        for (int h = 0; h < int(sizeof(e)) / 16; ++h) {
+          const W w = __builtin_nontemporal_load(as<const W>(p) + h);
+          __builtin_memcpy(reinterpret_cast<char *>(e) + 16 * h, &w, 16);
+        }
       } else {
         __builtin_memcpy(e, p, sizeof(e));
       }
@@ -78,11 +81,14 @@ struct Vec {
   template <Move M = Move::kCached>
   __device__ __forceinline__ void store(T *p, int n) const {
     if (n >= V) {
-      if constexpr (M == Move::kStreamed && sizeof(e) == 16) {
+      if constexpr (M == Move::kStreamed && sizeof(e) % 16 == 0) {
         typedef unsigned int W __attribute__((ext_vector_type(4), aligned(2)));
-        W w;
-        __builtin_memcpy(&w, e, sizeof(e));
-        __builtin_nontemporal_store(w, as<W>(p));
+#pragma unroll
+        for (int h = 0; h < int(sizeof(e)) / 16; ++h) {
+          W w;
+          __builtin_memcpy(&w, reinterpret_cast<const char *>(e) + 16 * h, 16);
+          __builtin_nontemporal_store(w, as<W>(p) + h);
+        }
       } else {
         __builtin_memcpy(p, e, sizeof(e));
       }

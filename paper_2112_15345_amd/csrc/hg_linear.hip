@@ -251,12 +251,12 @@ __device__ __forceinline__ void with_act(int act, F f) {
     f(std::integral_constant<int, HG_ACT_RELU>());
 }
 
-template <typename T, int N>
+template <typename T, int N, Move M = Move::kCached>
 __device__ __forceinline__ void put(void *base, int64_t at, const float *v, int n) {
   Vec<T, N> t;
 #pragma unroll
   for (int j = 0; j < N; ++j) t.e[j] = T(v[j]);
-  t.store(static_cast<T *>(base) + at, n);
+  t.template store<M>(static_cast<T *>(base) + at, n);
 }
 template <int N>
 __device__ __forceinline__ void put_as(void *base, int32_t dtype, int64_t at, const float *v,
@@ -307,7 +307,7 @@ template <typename O, bool kPlain>
 __device__ __forceinline__ void finish(const Epilogue &E, const Columns &C, int64_t i,
                                        const Vec<O, 8> &residual, float *v) {
   if (kPlain) {
-    put<O, 8>(E.y, i * E.y_stride + C.j, v, C.n);
+    put<O, 8, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
     return;
   }
   if (E.col_scale) {
@@ -319,7 +319,7 @@ __device__ __forceinline__ void finish(const Epilogue &E, const Columns &C, int6
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += C.bias[k];
   }
-  if (E.pre) put<O, 8>(E.pre, i * E.pre_stride + C.j, v, C.n);
+  if (E.pre) put<O, 8, Move::kStreamed>(E.pre, i * E.pre_stride + C.j, v, C.n);
   with_act(E.act, [&](auto act) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = act_of<decltype(act)::value>(v[k]);
@@ -328,7 +328,7 @@ __device__ __forceinline__ void finish(const Epilogue &E, const Columns &C, int6
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += float(residual.e[k]);
   }
-  put<O, 8>(E.y, i * E.y_stride + C.j, v, C.n);
+  put<O, 8, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
 }
 template <typename O>
 __device__ __forceinline__ void load_residual(const Epilogue &E, const Columns &C, int64_t i,
@@ -470,14 +470,17 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
     for (int b = 0; b < NJ; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   constexpr int LP = SP::kTotal / 256, LQ = SQ::kTotal / 256;
-  for (int64_t q = q_begin; q < q_end; q += kDepth<T, 128>) {
-    u32x4 vp[LP], vq[LQ];
+  u32x4 vp[LP], vq[LQ];
+  const auto load = [&](int64_t q) {
 #pragma unroll
-    for (int u = 0; u < LP; ++u) 
+    for (int u = 0; u < LP; ++u)
       vp[u] = load_piece<S, SP, TP>(A.P, j0, q, q_end, u * 256 + threadIdx.x);
 #pragma unroll
-    for (int u = 0; u < LQ; ++u) 
+    for (int u = 0; u < LQ; ++u)
       vq[u] = load_piece<S, SQ, TQ>(A.Q, i0, q, q_end, u * 256 + threadIdx.x);
+  };
+  if (q_begin < q_end) load(q_begin);
+  for (int64_t q = q_begin; q < q_end; q += kDepth<T, 128>) {
     __syncthreads();  // the last slab has been read
 #pragma unroll
     for (int u = 0; u < LP; ++u) {
@@ -491,6 +494,7 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
                                  SQ::piece(t / SQ::kRowPieces, t % SQ::kRowPieces)) = vq[u];
     }
     __syncthreads();
+    if (q + kDepth<T, 128> < q_end) load(q + kDepth<T, 128>);  // in flight meanwhile
     u32x4 fp[NJ][2], fq[NI][2];
 #pragma unroll
     for (int b = 0; b < NJ; ++b) SP::fragments(lds, wj + 16 * b, fp[b]);
@@ -654,27 +658,133 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
 }
 
-// Adds the parts of a product in order, then the epilogue.
+// Adds the parts of a product in a fixed order, then the epilogue.  kShare threads share 8
+// neighbours of a row: each adds every kShare-th part, the first adds theirs.
+template <int kShare>
 __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
+  constexpr int kAt = 256 / kShare;
+  __shared__ float red[kShare > 1 ? kShare : 1][kShare > 1 ? kAt : 1][9];
   const int64_t per_row = (E.cols + 7) / 8;
-  const int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (t >= E.rows * per_row) return;
-  const int64_t i = t / per_row, j = t % per_row * 8;
+  const int share = threadIdx.x / kAt, at = threadIdx.x % kAt;
+  const int64_t t = int64_t(blockIdx.x) * kAt + at;
+  const bool in = t < E.rows * per_row;
+  const int64_t i = in ? t / per_row : 0, j = in ? t % per_row * 8 : 0;
   float *const part = E.part;
   E.part = nullptr;
   const Columns C(E, j);
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int s = 0; s < splits; ++s) {
+#pragma unroll 4
+  for (int s = share; s < splits; s += kShare) {
     float a[8];
     get<float, 8>(part, (s * E.rows + i) * E.cols + j, a, C.n);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += a[k];
   }
+  if constexpr (kShare > 1) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) red[share][at][k] = v[k];
+    __syncthreads();
+    if (share) return;
+    for (int s = 1; s < kShare; ++s)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += red[s][at][k];
+  }
+  if (!in) return;
   with_type(E.dtype, [&](auto type) {
     Vec<decltype(type), 8> r;
     load_residual(E, C, i, r);
     finish<decltype(type), false>(E, C, i, r, v);
   });
+}
+
+// ---- few rows ------------------------------------------------------------------
+
+// Products of at most kFew rows: bound by reading w once.  A wavefront takes 16 rows of w
+// (columns of C) and every kWaves-th 128 bytes of them, straight from memory into the
+// matrix instructions' registers, several loads ahead; a block's wavefronts are added in
+// LDS.  G: 16-row parts of x.
+constexpr int64_t kFew = 32;
+
+// 16 bytes of a row of n elements from element c on; zeros past its end.
+template <typename S>
+__device__ __forceinline__ u32x4 row_piece(const S *row, int64_t c, int64_t n) {
+  constexpr int E = 16 / int(sizeof(S));
+  u32x4 v = {0, 0, 0, 0};
+  if (c + E <= n) {
+    __builtin_memcpy(&v, row + c, 16);
+  } else if (c < n) {
+    S e[E];
+    __builtin_memset(e, 0, 16);
+    for (int k = 0; k < E; ++k)
+      if (c + k < n) e[k] = row[c + k];
+    __builtin_memcpy(&v, e, 16);
+  }
+  return v;
+}
+
+template <typename S, int G, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
+  constexpr int D = 128 / int(sizeof(S));  // elements of a step
+  constexpr int U = G == 1 ? 4 : 2;        // steps in flight
+  __shared__ float red[kWaves][G][16][20];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int g = lane >> 4, x = lane & 15;
+  const int64_t j0 = int64_t(blockIdx.x) * 16;
+  // past the end: results that are not written, any row will do
+  const S *const w = static_cast<const S *>(A.P.p) + min(j0 + x, A.P.rows - 1) * A.P.stride;
+  const S *rows[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i)
+    rows[i] = static_cast<const S *>(A.Q.p) + min<int64_t>(16 * i + x, A.Q.rows - 1) * A.Q.stride;
+  f32x4 acc[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t q0 = int64_t(blockIdx.y) * A.per_split;
+  const int64_t n = min(A.depth, q0 + A.per_split);
+  const int c = g * (16 / int(sizeof(S)));  // this lane's piece of 64 bytes
+  for (int64_t q = q0 + int64_t(wave) * D; q < n; q += int64_t(kWaves) * D * U) {
+    u32x4 fw[U][2], fx[U][G][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t at = q + int64_t(u) * kWaves * D + h * (D / 2) + c;
+        fw[u][h] = row_piece(w, at, n);
+#pragma unroll
+        for (int i = 0; i < G; ++i) fx[u][i][h] = row_piece(rows[i], at, n);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const Step<S> p(fw[u][h]);
+#pragma unroll
+        for (int i = 0; i < G; ++i) acc[i] = p.mma(Step<S>(fx[u][i][h]), acc[i]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < G; ++i)
+    *reinterpret_cast<f32x4 *>(&red[wave][i][x][4 * g]) = acc[i];
+  __syncthreads();
+  // 8 neighbours of a row each
+  for (int t = threadIdx.x; t < G * 32; t += 64 * kWaves) {
+    const int64_t i = t >> 1;
+    const Columns C(A.E, j0 + (t & 1) * 8);
+    if (i >= A.E.rows || C.n <= 0) continue;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int s = 0; s < kWaves; ++s)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
+    if (A.E.part) {
+      put<float, 8>(A.E.part, (int64_t(blockIdx.y) * A.E.rows + i) * A.E.cols + C.j, v, C.n);
+      continue;
+    }
+    with_type(A.E.dtype, [&](auto type) {
+      Vec<decltype(type), 8> r;
+      load_residual(A.E, C, i, r);
+      finish<decltype(type), false>(A.E, C, i, r, v);
+    });
+  }
 }
 
 // ---- dz and its column sums ------------------------------------------------------
@@ -736,25 +846,86 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, cons
 
 // ---- launches --------------------------------------------------------------------
 
-constexpr int kTile = 128;
-
 int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
 int64_t size_of(int32_t dtype) {
   return dtype == HG_DT_F32 ? 4 : (dtype == HG_DT_E4M3 ? 1 : 2);
 }
-int64_t depth_of(int32_t dtype) { return 128 / (dtype == HG_DT_F32 ? 4 : 2); }
+// Elements of q in 128 bytes of what the matrix instructions take.
+int64_t slab_of(int32_t dtype) { return dtype == HG_DT_F32 ? 32 : 64; }
 
-// Into how many parts the depth is cut: enough for two blocks on each of 256 compute
-// units, each of at least 8 slabs.
-int64_t splits_of(int64_t tiles, int64_t depth, int64_t slab) {
-  const int64_t want = tiles < 512 ? 512 / tiles : 1;
-  const int64_t most = depth / (8 * slab);
-  const int64_t s = want < most ? want : most;
-  return s < 1 ? 1 : (s > 256 ? 256 : s);
+// How a product is cut: its tiles, how many slabs are in LDS, and the parts of its depth.
+// A compute unit that multiplies one tile waits for its loads unless several slabs are in
+// flight; with two tiles each covers the other's waits.
+//  kLarge   256 x 256, 2 slabs, one block on a unit: 1.28 PF/s in 16 bits at 8192^3.  Not
+//           for depths below 8 slabs (150001 x 128 x 256: 36 us, kMedium 33) nor in 32 bits,
+//           whose products take too long for its uneven last round
+//  kMedium  128 x 128, 2 slabs, two blocks: loading a slab takes as long as multiplying it
+//           (64 bytes a clock), 1.0 PF/s at 8192^3, but its tiles fill the units better
+//  kSmall   64 x 64, 4 slabs, two blocks: for too few tiles of the others (1024^3: 8.8 us,
+//           kMedium 18), unless the depth is long enough to be cut (rows of 512 and 1024
+//           columns' gradient over 65537 rows: 172 us, kMedium 112)
+//  kTall    256 x 128 in slabs of 64 bytes, two blocks: the weight gradients' operands,
+//           whose slabs are read across (8192^3: 1.20 PF/s, kLarge 1.11, kMedium 1.04)
+enum class Cut { kLarge, kMedium, kSmall, kTall };
+struct Plan {
+  Cut cut;
+  int64_t tile_i, tile_j, splits, per_split;
+  int64_t rows;  // of C that this plan is for; the rest have one of their own
+};
+constexpr int64_t kUnits = 256;
+
+int64_t tiles_of(int64_t rows, int64_t cols, int64_t ti, int64_t tj) {
+  return ceil_div<int64_t>(rows, ti) * ceil_div<int64_t>(cols, tj);
 }
-int64_t splits_for(int64_t rows, int64_t cols, int64_t depth, int64_t slab) {
-  if (rows <= 0 || cols <= 0) return 1;
-  return splits_of(ceil_div<int64_t>(rows, kTile) * ceil_div<int64_t>(cols, kTile), depth, slab);
+// The share of the last round of blocks that is full, over all rounds.
+double filled(int64_t tiles, int64_t at_once) {
+  return double(tiles) / double(ceil_div<int64_t>(tiles, at_once) * at_once);
+}
+
+Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both) {
+  Plan p{Cut::kMedium, 128, 128, 1, 0, rows};
+  if (rows > 0 && cols > 0) {
+    const int64_t large = tiles_of(rows, cols, 256, 256), tall = tiles_of(rows, cols, 256, 128);
+    const int64_t medium = tiles_of(rows, cols, 128, 128);
+    if (both && tall >= kUnits)
+      p = Plan{Cut::kTall, 256, 128, 1, 0, rows};
+    else if (!both && large >= 2 * kUnits && depth >= 8 * slab && slab == 64)
+      p = Plan{Cut::kLarge, 256, 256, 1, 0, rows};
+    else if (medium <= kUnits / 2 && medium * (depth / (32 * slab)) <= kUnits / 2)
+      p = Plan{Cut::kSmall, 64, 64, 1, 0, rows};
+    const int64_t at_once = p.cut == Cut::kLarge ? kUnits : 2 * kUnits;
+    const int64_t tiles = tiles_of(rows, cols, p.tile_i, p.tile_j);
+    if (tiles < at_once) {
+      // the depth in parts of at least 8 slabs; where half the blocks are there anyway, only
+      // a depth that is long next to the writing and adding of the parts
+      const int64_t long_ = p.cut == Cut::kSmall ? 16 * slab : 64 * slab;
+      const int64_t least = 2 * tiles >= at_once ? long_ : 8 * slab;
+      const int64_t want = at_once / tiles, most = depth / least;
+      p.splits = want < most ? want : most;
+      if (p.splits > 256) p.splits = 256;
+      if (p.splits < 1) p.splits = 1;
+    } else if (tiles <= 6 * at_once && filled(tiles, at_once) < 0.9 && depth >= 16 * slab) {
+      // the rows of whole rounds; the last round's few tiles would leave most units idle
+      // for as long as a full one takes, and are cut finer
+      const int64_t down = tiles / at_once * at_once / ceil_div<int64_t>(cols, p.tile_j);
+      if (down > 0) p.rows = down * p.tile_i;
+    }
+  }
+  p.per_split = ceil_div<int64_t>(ceil_div<int64_t>(depth, slab), p.splits) * slab;
+  if (p.per_split < slab) p.per_split = slab;
+  p.splits = depth > 0 ? ceil_div<int64_t>(depth, p.per_split) : 1;
+  return p;
+}
+// Bytes of the parts of a product, its rows taken plan by plan.
+int64_t parts_bytes(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both) {
+  int64_t most = 0;
+  while (rows > 0 && cols > 0) {
+    const Plan p = plan_of(rows, cols, depth, slab, both);
+    const int64_t bytes = p.splits > 1 ? p.splits * p.rows * cols * 4 : 0;
+    most = bytes > most ? bytes : most;
+    rows -= p.rows;
+  }
+  return most;
 }
 
 // Whether every 16-byte piece of an operand is aligned, and lies in it or outside it.
@@ -763,6 +934,70 @@ bool is_direct(const Operand &O, bool turned, int64_t depth) {
   constexpr int64_t E = 16 / int64_t(sizeof(S));
   return reinterpret_cast<uintptr_t>(O.p) % 16 == 0 && O.stride % E == 0 &&
          (turned ? O.rows : depth) % E == 0;
+}
+
+template <typename S, bool TP, bool TQ, int BI, int BJ, int kWavesI, int kWavesJ, int W,
+          int kStages>
+void launch_direct(const Product &A, dim3 grid, hipStream_t stream) {
+  hipLaunchKernelGGL((k_product_direct<S, TP, TQ, BI, BJ, kWavesI, kWavesJ, W, kStages>), grid,
+                     dim3(64 * kWavesI * kWavesJ), 0, stream, A);
+}
+
+// Few rows: blocks of 4 wavefronts, or of 16 where there are few columns; with very few,
+// the depth is cut too, in parts of at least two steps of 128 bytes for a wavefront.
+struct FewPlan {
+  int64_t blocks, waves, splits, per_split;
+};
+FewPlan few_plan(int64_t cols, int64_t depth, int64_t size) {
+  FewPlan p;
+  p.blocks = ceil_div<int64_t>(cols, 16);
+  p.waves = p.blocks >= 512 ? 4 : 16;
+  const int64_t step = p.waves * (128 / size);
+  const int64_t want = p.blocks < 128 && p.blocks > 0 ? 256 / p.blocks : 1;
+  const int64_t most = depth / (2 * step);
+  p.splits = want < most ? want : most;
+  if (p.splits < 1) p.splits = 1;
+  p.per_split = ceil_div<int64_t>(ceil_div<int64_t>(depth, step), p.splits) * step;
+  if (p.per_split < step) p.per_split = step;
+  p.splits = depth > 0 ? ceil_div<int64_t>(depth, p.per_split) : 1;
+  return p;
+}
+
+template <typename S, int G>
+void launch_few(const Product &A, const FewPlan &p, hipStream_t stream) {
+  const dim3 grid(unsigned(p.blocks), unsigned(p.splits));
+  if (p.waves == 4)
+    hipLaunchKernelGGL((k_few<S, G, 4>), grid, dim3(256), 0, stream, A);
+  else
+    hipLaunchKernelGGL((k_few<S, G, 16>), grid, dim3(1024), 0, stream, A);
+}
+
+hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
+  const int64_t vectors = E.rows * ceil_div<int64_t>(E.cols, 8);
+  if (splits > 4)
+    hipLaunchKernelGGL(k_join<8>, dim3(unsigned(ceil_div<int64_t>(vectors, 32))), dim3(256), 0,
+                       stream, E, int32_t(splits));
+  else
+    hipLaunchKernelGGL(k_join<1>, dim3(unsigned(ceil_div<int64_t>(vectors, 256))), dim3(256), 0,
+                       stream, E, int32_t(splits));
+  return hipGetLastError();
+}
+
+// The operand, and the epilogue, of n rows of C from row `at` on.
+template <typename S>
+Operand rows_from(Operand Q, bool turned, int64_t at, int64_t n) {
+  Q.p = static_cast<const S *>(Q.p) + (turned ? at : at * Q.stride);
+  Q.rows = n;
+  return Q;
+}
+Epilogue epilogue_from(Epilogue E, int64_t at, int64_t n) {
+  const int64_t size = size_of(E.dtype);
+  E.rows = n;
+  E.y = static_cast<char *>(E.y) + at * E.y_stride * size;
+  if (E.residual) E.residual = static_cast<const char *>(E.residual) + at * E.residual_stride * size;
+  if (E.pre) E.pre = static_cast<char *>(E.pre) + at * E.pre_stride * size;
+  if (E.row_scale) E.row_scale += at;
+  return E;
 }
 
 template <typename S, bool TP, bool TQ>
@@ -774,47 +1009,53 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
   A.Q = Q;
   A.depth = depth;
   A.E = E;
-  const int64_t ti = ceil_div<int64_t>(E.rows, kTile), tj = ceil_div<int64_t>(E.cols, kTile);
-  if (ti * tj >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
-  A.tiles_i = int32_t(ti);
-  A.tiles_j = int32_t(tj);
-  const int64_t slab = kDepth<typename ComputeOf<S>::T, 128>;
-  int64_t splits = parts ? splits_for(E.rows, E.cols, depth, slab) : 1;
-  A.per_split = ceil_div<int64_t>(ceil_div<int64_t>(depth, slab), splits) * slab;
-  if (A.per_split < slab) A.per_split = slab;
-  splits = depth > 0 ? ceil_div<int64_t>(depth, A.per_split) : 1;
-  if (splits > 1) A.E.part = parts;
-  const dim3 grid(unsigned(ti * tj), unsigned(splits));
-  const bool direct = is_direct<S>(P, TP, depth) && is_direct<S>(Q, TQ, depth);
-#ifndef HG_TI
-#define HG_TI 128
-#define HG_TJ 128
-#define HG_WI 2
-#define HG_WJ 2
-#define HG_W 128
-#define HG_ST 2
-#endif
-  {
-    if (direct) {
-      A.tiles_i = int32_t(ceil_div<int64_t>(E.rows, HG_TI));
-      A.tiles_j = int32_t(ceil_div<int64_t>(E.cols, HG_TJ));
-      hipLaunchKernelGGL((k_product_direct<S, TP, TQ, HG_TI, HG_TJ, HG_WI, HG_WJ, HG_W, HG_ST>), dim3(unsigned(A.tiles_i)*unsigned(A.tiles_j), unsigned(splits)), dim3(HG_WI*HG_WJ*64), 0,
-                         stream, A);
+  if constexpr (!TP && !TQ) {
+    if (E.rows <= kFew) {
+      const FewPlan p = few_plan(E.cols, depth, sizeof(S));
+      A.per_split = p.per_split;
+      if (p.splits > 1) A.E.part = parts;
+      if (E.rows <= 16)
+        launch_few<S, 1>(A, p, stream);
+      else
+        launch_few<S, 2>(A, p, stream);
+      const hipError_t e = hipGetLastError();
+      return e != hipSuccess || p.splits == 1 ? e : join(A.E, p.splits, stream);
     }
   }
-  if (!direct)
-    hipLaunchKernelGGL((k_product<S, TP, TQ, kTile, kTile>), grid, dim3(256), 0, stream, A);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
-  const int64_t threads = E.rows * ceil_div<int64_t>(E.cols, 8);
-  hipLaunchKernelGGL(k_join, dim3(unsigned(ceil_div<int64_t>(threads, 256))), dim3(256), 0, stream,
-                     A.E, int32_t(splits));
-  return hipGetLastError();
-}
-
-int64_t parts_bytes(int64_t rows, int64_t cols, int64_t depth, int64_t slab) {
-  const int64_t s = splits_for(rows, cols, depth, slab);
-  return s > 1 ? s * rows * cols * 4 : 0;
+  const int64_t slab = kDepth<typename ComputeOf<S>::T, 128>;
+  const bool direct = is_direct<S>(P, TP, depth) && is_direct<S>(Q, TQ, depth);
+  for (int64_t done = 0; done < E.rows;) {
+    Plan p = plan_of(E.rows - done, E.cols, depth, slab, TP && TQ);
+    // (any operands: tiles of 128 x 128 or 64 x 64; the parts and rows stay as planned)
+    if (!direct && p.cut != Cut::kSmall) p.cut = Cut::kMedium, p.tile_i = p.tile_j = 128;
+    Product B = A;
+    B.Q = rows_from<S>(Q, TQ, done, p.rows);
+    B.E = epilogue_from(E, done, p.rows);
+    const int64_t ti = ceil_div<int64_t>(p.rows, p.tile_i), tj = ceil_div<int64_t>(E.cols, p.tile_j);
+    if (ti * tj >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
+    B.tiles_i = int32_t(ti);
+    B.tiles_j = int32_t(tj);
+    B.per_split = p.per_split;
+    if (p.splits > 1) B.E.part = parts;
+    const dim3 grid(unsigned(ti * tj), unsigned(p.splits));
+    if (!direct && p.cut == Cut::kSmall)
+      hipLaunchKernelGGL((k_product<S, TP, TQ, 64, 64>), grid, dim3(256), 0, stream, B);
+    else if (!direct)
+      hipLaunchKernelGGL((k_product<S, TP, TQ, 128, 128>), grid, dim3(256), 0, stream, B);
+    else if (p.cut == Cut::kMedium)
+      launch_direct<S, TP, TQ, 128, 128, 2, 2, 128, 2>(B, grid, stream);
+    else if (p.cut == Cut::kSmall)
+      launch_direct<S, TP, TQ, 64, 64, 2, 2, 128, 4>(B, grid, stream);
+    else if constexpr (TP && TQ)
+      launch_direct<S, TP, TQ, 256, 128, 4, 2, 64, 3>(B, grid, stream);
+    else
+      launch_direct<S, TP, TQ, 256, 256, 2, 4, 128, 2>(B, grid, stream);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && p.splits > 1) e = join(B.E, p.splits, stream);
+    if (e != hipSuccess) return e;
+    done += p.rows;
+  }
+  return hipSuccess;
 }
 
 template <typename T>
@@ -845,11 +1086,11 @@ struct GradSpace {  // byte offsets in the workspace
 };
 GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
   GradSpace g;
-  const int64_t slab = depth_of(dtype);
+  const int64_t slab = slab_of(dtype);
   g.dz = 0;
   g.sums = align16(act == HG_ACT_NONE ? 0 : m * n * size_of(dtype));
   g.parts = g.sums + align16(ceil_div<int64_t>(m, kSumRows) * n * 4);
-  const int64_t a = parts_bytes(m, k, n, slab), b = parts_bytes(n, k, m, slab);
+  const int64_t a = parts_bytes(m, k, n, slab, false), b = parts_bytes(n, k, m, slab, true);
   g.total = g.parts + align16(a > b ? a : b);
   return g;
 }
@@ -912,7 +1153,11 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
 }  // namespace
 
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {
-  return parts_bytes(m, n, k, depth_of(dtype));
+  if (m <= kFew) {
+    const int64_t splits = few_plan(n, k, size_of(dtype)).splits;
+    return splits > 1 ? splits * m * n * 4 : 0;
+  }
+  return parts_bytes(m, n, k, slab_of(dtype), false);
 }
 
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream) {
