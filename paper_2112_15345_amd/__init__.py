@@ -197,6 +197,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         views = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(views)
         views.bind(*_accessors(lib))
+        views.bind_dense(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.hg_rms_norm, lib.hg_rms_norm_grad, lib.hg_rms_norm_grad_workspace, lib.hg_linear,
+            lib.hg_linear_workspace, lib.hg_linear_grad, lib.hg_linear_grad_workspace,
+            lib.hg_distill)))
         _views = views
         _lib = lib
     return _lib

@@ -63,13 +63,14 @@ def _build_views(verbose: bool) -> None:
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-D__HIP_PLATFORM_AMD__=1", "-I", INCLUDE, *inc,
-           os.path.join(CSRC, "hg_views.cpp"), "-o", tmp, "-L", libdir, "-ltorch", "-ltorch_cpu",
-           "-lc10", "-ltorch_python", f"-Wl,-rpath,{libdir}"]
+           os.path.join(CSRC, "hg_views.cpp"), os.path.join(CSRC, "hg_dense_py.cpp"), "-o", tmp,
+           "-L", libdir, "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip", "-ltorch_python",
+           f"-Wl,-rpath,{libdir}"]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError(f"g++ failed on hg_views.cpp:\n{res.stdout}\n{res.stderr}")
+        raise RuntimeError(f"g++ failed on hg_views.cpp, hg_dense_py.cpp:\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, VIEWS_PATH)
 
 
