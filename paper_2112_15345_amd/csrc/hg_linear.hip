@@ -74,25 +74,115 @@ __device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, float) {
   return c;
 }
 
-// A fragment as the matrix instructions take it.
-template <typename S>
+struct Plain32 {};
+
+// Fragments as the matrix instructions take them, kPer of them at a time.
+template <typename S, bool kExact>
 struct Step {
+  static constexpr int kPer = 1;
   u32x4 v;
   __device__ __forceinline__ Step() {}
-  __device__ __forceinline__ explicit Step(u32x4 f) : v(f) {}
+  __device__ __forceinline__ explicit Step(const u32x4 *f) : v(f[0]) {}
   __device__ __forceinline__ f32x4 mma(const Step &q, f32x4 c) const {
     return hg::mma(c, v, q.v, S());
   }
 };
-template <>
-struct Step<F8> {  // 16 elements: two steps of bfloat16
+template <bool kExact>
+struct Step<F8, kExact> {  // 16 elements: two steps of bfloat16
+  static constexpr int kPer = 1;
   u32x4 v[2];
   __device__ __forceinline__ Step() {}
-  __device__ __forceinline__ explicit Step(u32x4 f)
-      : v{widen(u32x2{f[0], f[1]}), widen(u32x2{f[2], f[3]})} {}
+  __device__ __forceinline__ explicit Step(const u32x4 *f)
+      : v{widen(u32x2{f[0][0], f[0][1]}), widen(u32x2{f[0][2], f[0][3]})} {}
   __device__ __forceinline__ f32x4 mma(const Step &q, f32x4 c) const {
     c = hg::mma(c, v[0], q.v[0], __bf16());
     return hg::mma(c, v[1], q.v[1], __bf16());
+  }
+};
+// 32-bit elements as three bfloat16 that add up to them exactly, x = h + m + l with h rounded
+// to nearest, |m| <= 2^-9 |x| and |l| <= 2^-16 |x|: six products of theirs give the product
+// of two elements within 2^-24 of its size (m l, l m and l l are left out), and the 16-bit
+// instructions are 16 times as fast as the 32-bit ones (16385 x 1024 x 4096: 771 us, by the
+// 32-bit instructions 1303).  The pieces are made by integer operations: the conversion
+// instruction is slower than the products it feeds (881 us with it).
+// Infinities and values that round past the largest bfloat16 give NaN pieces, and so a
+// NaN in the result: the caller then starts again with kExact, where those values are one
+// piece (h; nothing in the products of the smaller pieces, where an infinity would meet
+// zeros).  Finite values have the same pieces either way, so that what a NaN does not
+// reach keeps its bits.
+template <bool kExact>
+struct Step<float, kExact> {
+  static constexpr int kPer = 2;
+  u32x4 h, m, l, g;  // g: h of the finite values
+  __device__ __forceinline__ Step() {}
+  __device__ __forceinline__ explicit Step(const u32x4 *f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // two elements to a register of each piece
+      const uint32_t x = f[e / 2][e % 2 * 2], y = f[e / 2][e % 2 * 2 + 1];
+      uint32_t hx = (x + 0x8000u) & 0xffff0000u, hy = (y + 0x8000u) & 0xffff0000u;
+      float rx = __uint_as_float(x) - __uint_as_float(hx);
+      float ry = __uint_as_float(y) - __uint_as_float(hy);
+      uint32_t gx = hx, gy = hy;
+      if (kExact) {
+        careful(x, hx, rx, gx);
+        careful(y, hy, ry, gy);
+      }
+      h[e] = upper(hx, hy);
+      g[e] = kExact ? upper(gx, gy) : h[e];
+      const uint32_t mx = __float_as_uint(rx) & 0xffff0000u, my = __float_as_uint(ry) & 0xffff0000u;
+      m[e] = upper(__float_as_uint(rx), __float_as_uint(ry));
+      l[e] = upper(__float_as_uint(rx - __uint_as_float(mx)),
+                   __float_as_uint(ry - __uint_as_float(my)));
+    }
+  }
+  // The upper halves of two values, as two bfloat16.
+  __device__ __forceinline__ static uint32_t upper(uint32_t x, uint32_t y) {
+    return __builtin_amdgcn_perm(y, x, 0x07060302u);
+  }
+  // h, x - h and g of a value that may not be finite or may round to an infinity.
+  __device__ __forceinline__ static void careful(uint32_t x, uint32_t &h, float &r, uint32_t &g) {
+    const uint32_t size = x & 0x7fffffffu;
+    if (size >= 0x7f800000u) {  // (a NaN's own bits: rounding may carry them away)
+      h = size > 0x7f800000u ? 0x7fc00000u : x;
+      r = 0.0f;
+      g = 0;
+    } else {
+      if ((h & 0x7fffffffu) >= 0x7f800000u) h = x & 0xffff0000u;
+      r = __uint_as_float(x) - __uint_as_float(h);
+      g = h;
+    }
+  }
+};
+
+// One row of 16 x 16 parts.  (32 bits: product by product over the row, since an
+// instruction that adds to what the last one has not finished waits for it.)
+template <typename St, int NJ>
+__device__ __forceinline__ void mma_row(const St (&p)[NJ], const St &q, f32x4 (&c)[NJ]) {
+  if constexpr (St::kPer == 2) {
+    const auto all = [&](u32x4 St::*a, u32x4 b) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) c[j] = mma(c[j], p[j].*a, b, __bf16());
+    };
+    all(&St::l, q.g);
+    all(&St::g, q.l);
+    all(&St::m, q.m);
+    all(&St::m, q.g);
+    all(&St::g, q.m);
+    all(&St::h, q.h);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) c[j] = p[j].mma(q, c[j]);
+  }
+}
+// 64 x 64 tiles of 32-bit elements, where latency counts, use the 32-bit instructions.
+template <>
+struct Step<Plain32, true> {
+  static constexpr int kPer = 1;
+  u32x4 v;
+  __device__ __forceinline__ Step() {}
+  __device__ __forceinline__ explicit Step(const u32x4 *f) : v(f[0]) {}
+  __device__ __forceinline__ f32x4 mma(const Step &q, f32x4 c) const {
+    return hg::mma(c, v, q.v, float());
   }
 };
 
@@ -584,6 +674,7 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   using LP = Stream<S, TP, BJ, W, kWaves>;
   using LQ = Stream<S, TQ, BI, W, kWaves>;
   constexpr int kFrags = W / 64;
+  constexpr bool kPlain32 = sizeof(S) == 4 && BI < 128;
   constexpr int kStage = SP::kBytes + SQ::kBytes;
   constexpr int kOut = kWaves * 16 * (WJ + 4) * 4;
   static_assert(kOut <= kStages * kStage, "the parts of C fit where the slabs were");
@@ -598,61 +689,76 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   const int slabs = whole + (rest > 0);
   const int wi = wave / kWavesJ * WI, wj = wave % kWavesJ * WJ;
 
-  f32x4 acc[NI][NJ];
-#pragma unroll
-  for (int a = 0; a < NI; ++a)
-#pragma unroll
-    for (int b = 0; b < NJ; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  LP lp;
-  LQ lq;
-  lp.begin(A.P, j0, q_begin);
-  lq.begin(A.Q, i0, q_begin);
-  const auto load = [&](int slab, char *to) {
-    if (slab < whole) {
-      lp.template load<true>(to, 0);
-      lq.template load<true>(to + SP::kBytes, 0);
-    } else if (slab < slabs) {
-      lp.template load<false>(to, rest);
-      lq.template load<false>(to + SP::kBytes, rest);
-    }
-  };
-#pragma unroll
-  for (int u = 0; u < kStages - 1; ++u) load(u, lds + u * kStage);
-  int now = 0, ahead = kStages - 1;  // places in the ring
   const bool idle = i0 + wi >= A.E.rows || j0 + wj >= A.E.cols;  // no part of C for this wavefront
-  for (int slab = 0; slab < slabs; ++slab) {
-    // this wavefront's loads of the slab have landed (those of later ones may be in flight)
-    if (slab + kStages - 1 <= slabs)
-      wait_loads<(kStages - 2) * (LP::kLoads + LQ::kLoads)>();
-    else
-      wait_loads<0>();
-    // now everyone's have, and the slab that the next loads overwrite has been read
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    load(slab + kStages - 1, lds + ahead * kStage);
-    const char *const at = lds + now * kStage;
-    ahead = now;
-    now = now + 1 == kStages ? 0 : now + 1;
-    if (idle) continue;
-    u32x4 fp[NJ][kFrags], fq[NI][kFrags];
+
+  f32x4 acc[NI][NJ];
+  const auto multiply_all = [&](auto exact) {
+    typedef Step<std::conditional_t<kPlain32, Plain32, S>, decltype(exact)::value> St;
 #pragma unroll
-    for (int b = 0; b < NJ; ++b) SP::fragments(at, wj + 16 * b, fp[b]);
+    for (int a = 0; a < NI; ++a)
 #pragma unroll
-    for (int a = 0; a < NI; ++a) SQ::fragments(at + SP::kBytes, wi + 16 * a, fq[a]);
+      for (int b = 0; b < NJ; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    LP lp;
+    LQ lq;
+    lp.begin(A.P, j0, q_begin);
+    lq.begin(A.Q, i0, q_begin);
+    const auto load = [&](int slab, char *to) {
+      if (slab < whole) {
+        lp.template load<true>(to, 0);
+        lq.template load<true>(to + SP::kBytes, 0);
+      } else if (slab < slabs) {
+        lp.template load<false>(to, rest);
+        lq.template load<false>(to + SP::kBytes, rest);
+      }
+    };
 #pragma unroll
-    for (int h = 0; h < kFrags; ++h) {
-      Step<S> tp[NJ];
+    for (int u = 0; u < kStages - 1; ++u) load(u, lds + u * kStage);
+    int now = 0, ahead = kStages - 1;  // places in the ring
+    for (int slab = 0; slab < slabs; ++slab) {
+      // this wavefront's loads of the slab have landed (those of later ones may be in flight)
+      if (slab + kStages - 1 <= slabs)
+        wait_loads<(kStages - 2) * (LP::kLoads + LQ::kLoads)>();
+      else
+        wait_loads<0>();
+      // now everyone's have, and the slab that the next loads overwrite has been read
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      load(slab + kStages - 1, lds + ahead * kStage);
+      const char *const at = lds + now * kStage;
+      ahead = now;
+      now = now + 1 == kStages ? 0 : now + 1;
+      if (idle) continue;
+      u32x4 fp[NJ][kFrags], fq[NI][kFrags];
 #pragma unroll
-      for (int b = 0; b < NJ; ++b) tp[b] = Step<S>(fp[b][h]);
+      for (int b = 0; b < NJ; ++b) SP::fragments(at, wj + 16 * b, fp[b]);
 #pragma unroll
-      for (int a = 0; a < NI; ++a) {
-        const Step<S> tq(fq[a][h]);
+      for (int a = 0; a < NI; ++a) SQ::fragments(at + SP::kBytes, wi + 16 * a, fq[a]);
 #pragma unroll
-        for (int b = 0; b < NJ; ++b) acc[a][b] = tp[b].mma(tq, acc[a][b]);
+      for (int h = 0; h < kFrags; h += St::kPer) {
+        St tp[NJ];
+#pragma unroll
+        for (int b = 0; b < NJ; ++b) tp[b] = St(&fp[b][h]);
+#pragma unroll
+        for (int a = 0; a < NI; ++a) {
+          mma_row(tp, St(&fq[a][h]), acc[a]);
+        }
       }
     }
+  };
+  if constexpr (sizeof(S) == 4 && !kPlain32) {
+    multiply_all(std::false_type());
+    bool nan = false;
+#pragma unroll
+    for (int a = 0; a < NI; ++a)
+#pragma unroll
+      for (int b = 0; b < NJ; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) nan = nan || acc[a][b][e] != acc[a][b][e];
+    // (the barrier also says that the ring has been read)
+    if (__syncthreads_or(nan)) multiply_all(std::true_type());
+  } else {
+    multiply_all(std::true_type());
   }
   __syncthreads();
   write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
@@ -757,9 +863,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const Step<S> p(fw[u][h]);
+        if constexpr (sizeof(S) == 4) {  // (bound by memory: the 32-bit instructions are enough)
 #pragma unroll
-        for (int i = 0; i < G; ++i) acc[i] = p.mma(Step<S>(fx[u][i][h]), acc[i]);
+          for (int i = 0; i < G; ++i) acc[i] = mma(acc[i], fw[u][h], fx[u][i][h], S());
+        } else {
+          const Step<S, true> p(&fw[u][h]);
+#pragma unroll
+          for (int i = 0; i < G; ++i) acc[i] = p.mma(Step<S, true>(&fx[u][i][h]), acc[i]);
+        }
       }
   }
 #pragma unroll
@@ -887,7 +998,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both)
   if (rows > 0 && cols > 0) {
     const int64_t large = tiles_of(rows, cols, 256, 256), tall = tiles_of(rows, cols, 256, 128);
     const int64_t medium = tiles_of(rows, cols, 128, 128);
-    if (both && tall >= kUnits)
+    if (both && tall >= kUnits && slab == 64)
       p = Plan{Cut::kTall, 256, 128, 1, 0, rows};
     else if (!both && large >= 2 * kUnits && depth >= 8 * slab && slab == 64)
       p = Plan{Cut::kLarge, 256, 256, 1, 0, rows};
@@ -1046,6 +1157,8 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
       launch_direct<S, TP, TQ, 128, 128, 2, 2, 128, 2>(B, grid, stream);
     else if (p.cut == Cut::kSmall)
       launch_direct<S, TP, TQ, 64, 64, 2, 2, 128, 4>(B, grid, stream);
+    else if constexpr (sizeof(S) == 4)
+      return hipErrorInvalidConfiguration;  // (plan_of has no other cut in 32 bits)
     else if constexpr (TP && TQ)
       launch_direct<S, TP, TQ, 256, 128, 4, 2, 64, 3>(B, grid, stream);
     else
