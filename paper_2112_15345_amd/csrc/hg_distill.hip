@@ -417,56 +417,58 @@ __global__ __launch_bounds__(kBlockOf<G>) void k_distill(hg_distill_args A) {
   extern __shared__ float lds[];
   Row<T, G> R(A, lds, false);
   const int n = int(A.classes), tid = R.tid;
-  const int64_t i = int64_t(blockIdx.x) * kRowsOf<G> + threadIdx.x / G;
-  if (i >= A.rows) return;  // whole groups; with several a block there is no block barrier
-  const T *const z = static_cast<const T *>(A.logits) + i * A.logits_stride;
-  if (R.first()) {
-    R.fetch_list(i);
-    R.fetch_logits(i);
-  }
-  const Cut<T, kAlign> C(z, n);
-  const T *const body = z + C.head;
-  const int end = C.whole * V;
-  Softmax q;
-  int k0 = 0;
-  for (; k0 + G * V * U <= end; k0 += G * V * U) {
-    Vec<T> r[U];
-    float x[U * V];
+  // (a wavefront leaves on its own; a larger group is the block)
+  for (int64_t i = int64_t(blockIdx.x) * kRowsOf<G> + threadIdx.x / G; i < A.rows;
+       i += int64_t(gridDim.x) * kRowsOf<G>) {
+    const T *const z = static_cast<const T *>(A.logits) + i * A.logits_stride;
+    if (R.first()) {
+      R.fetch_list(i);
+      R.fetch_logits(i);
+    }
+    const Cut<T, kAlign> C(z, n);
+    const T *const body = z + C.head;
+    const int end = C.whole * V;
+    Softmax q;
+    int k0 = 0;
+    for (; k0 + G * V * U <= end; k0 += G * V * U) {
+      Vec<T> r[U];
+      float x[U * V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) r[u].template load<kMove>(body + k0 + (u * G + tid) * V, V);
+      for (int u = 0; u < U; ++u) r[u].template load<kMove>(body + k0 + (u * G + tid) * V, V);
 #pragma unroll
-    for (int u = 0; u < U * V; ++u) x[u] = float(r[u / V].e[u % V]);
-    q.add(x, R.c);
-  }
-  const auto add = [&](const T *p, int m) {
-    Vec<T> r;
-    float x[V];
-    r.template load<kMove>(p, m, T(-INFINITY));
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = float(r.e[j]);
-    q.add(x, R.c);
-  };
-  for (int k = k0 + tid * V; k < end; k += G * V) add(body + k, V);
-  if (kAlign && tid == 0 && C.head) add(z, C.head);
-  if (tid == 1 && C.last) add(z + n - C.last, C.last);
-  R.begin(i);
-  R.join(i, q);
-  if constexpr (kGrad) {
-    T *const grad = static_cast<T *>(A.grad) + i * A.grad_stride;
-    const bool zero = R.nothing || R.a == 0.0f;
-    const float f = R.a * R.inv_t / q.s;
-    const auto slope = [&](int k, int m) {
+      for (int u = 0; u < U * V; ++u) x[u] = float(r[u / V].e[u % V]);
+      q.add(x, R.c);
+    }
+    const auto add = [&](const T *p, int m) {
       Vec<T> r;
-      r.load(z + k, m);
+      float x[V];
+      r.template load<kMove>(p, m, T(-INFINITY));
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        r.e[j] = T(zero ? 0.0f : f * exp_of(float(r.e[j]), q.m, R.c));
-      r.template store<Move::kStreamed>(grad + k, m);
+      for (int j = 0; j < V; ++j) x[j] = float(r.e[j]);
+      q.add(x, R.c);
     };
-    for (int k = tid * V; k < end; k += G * V) slope(C.head + k, V);
-    if (tid == 0 && C.head) slope(0, C.head);
-    if (tid == 1 && C.last) slope(n - C.last, C.last);
-    R.listed_entries(grad, q);
+    for (int k = k0 + tid * V; k < end; k += G * V) add(body + k, V);
+    if (kAlign && tid == 0 && C.head) add(z, C.head);
+    if (tid == 1 && C.last) add(z + n - C.last, C.last);
+    R.begin(i);
+    R.join(i, q);
+    if constexpr (kGrad) {
+      T *const grad = static_cast<T *>(A.grad) + i * A.grad_stride;
+      const bool zero = R.nothing || R.a == 0.0f;
+      const float f = R.a * R.inv_t / q.s;
+      const auto slope = [&](int k, int m) {
+        Vec<T> r;
+        r.load(z + k, m);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          r.e[j] = T(zero ? 0.0f : f * exp_of(float(r.e[j]), q.m, R.c));
+        r.template store<Move::kStreamed>(grad + k, m);
+      };
+      for (int k = tid * V; k < end; k += G * V) slope(C.head + k, V);
+      if (tid == 0 && C.head) slope(0, C.head);
+      if (tid == 1 && C.last) slope(n - C.last, C.last);
+      R.listed_entries(grad, q);
+    }
   }
 }
 
@@ -484,8 +486,9 @@ hipError_t step(const hg_distill_args &A, hipStream_t stream) {
 template <typename T, int G, bool kGrad, bool kAlign>
 hipError_t sweep(const hg_distill_args &A, hipStream_t stream) {
   const size_t lds = size_t(kRowsOf<G>) * 2 * lds_floats<G>(A.top) * sizeof(float);
+  const int64_t blocks = ceil_div<int64_t>(A.rows, kRowsOf<G>);
   hipLaunchKernelGGL((k_distill<T, G, kGrad, kAlign>),
-                     dim3(unsigned(ceil_div<int64_t>(A.rows, kRowsOf<G>))), dim3(kBlockOf<G>), lds,
+                     dim3(unsigned(blocks < 65536 ? blocks : 65536)), dim3(kBlockOf<G>), lds,
                      stream, A);
   return hipGetLastError();
 }

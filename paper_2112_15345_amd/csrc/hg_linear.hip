@@ -1054,6 +1054,9 @@ void launch_direct(const Product &A, dim3 grid, hipStream_t stream) {
                      dim3(64 * kWavesI * kWavesJ), 0, stream, A);
 }
 
+// (A grid has fewer than 2^32 threads.)
+bool is_few(int64_t rows, int64_t cols) { return rows <= kFew && cols <= int64_t(1) << 26; }
+
 // Few rows: blocks of 4 wavefronts, or of 16 where there are few columns; with very few,
 // the depth is cut too, in parts of at least two steps of 128 bytes for a wavefront.
 struct FewPlan {
@@ -1121,7 +1124,7 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
   A.depth = depth;
   A.E = E;
   if constexpr (!TP && !TQ) {
-    if (E.rows <= kFew) {
+    if (is_few(E.rows, E.cols)) {
       const FewPlan p = few_plan(E.cols, depth, sizeof(S));
       A.per_split = p.per_split;
       if (p.splits > 1) A.E.part = parts;
@@ -1143,7 +1146,7 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
     B.Q = rows_from<S>(Q, TQ, done, p.rows);
     B.E = epilogue_from(E, done, p.rows);
     const int64_t ti = ceil_div<int64_t>(p.rows, p.tile_i), tj = ceil_div<int64_t>(E.cols, p.tile_j);
-    if (ti * tj >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
+    if (ti * tj * 512 >= int64_t(1) << 32) return hipErrorInvalidConfiguration;  // threads of a grid
     B.tiles_i = int32_t(ti);
     B.tiles_j = int32_t(tj);
     B.per_split = p.per_split;
@@ -1219,7 +1222,7 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
   const bool products = (A.dx || A.dw) && A.k > 0;
   if (A.m > 0 && A.n > 0 && ((has_act && products) || A.dbias)) {
     const int64_t strips = ceil_div<int64_t>(A.n, 512);
-    if (strips * chunks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
+    if (strips * chunks * 256 >= int64_t(1) << 32) return hipErrorInvalidConfiguration;
     T *const to = has_act && products ? reinterpret_cast<T *>(ws + g.dz) : nullptr;
     float *const sums = A.dbias ? reinterpret_cast<float *>(ws + g.sums) : nullptr;
     hipLaunchKernelGGL((k_dz<T>), dim3(unsigned(strips * chunks)), dim3(256), 0, stream,
@@ -1266,7 +1269,7 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
 }  // namespace
 
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {
-  if (m <= kFew) {
+  if (is_few(m, n)) {
     const int64_t splits = few_plan(n, k, size_of(dtype)).splits;
     return splits > 1 ? splits * m * n * 4 : 0;
   }

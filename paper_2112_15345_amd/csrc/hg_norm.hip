@@ -255,56 +255,57 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
   constexpr int V = kVec<T>;
   __shared__ float red[Group<kBlock>::kLds];
   Group<kBlock> grp(red);
-  const int64_t i = blockIdx.x;
   const int dim = int(A.dim);
-  const int64_t at = Source{A.ids, A.x_rows}.at(i);
-  auto load_h = [&](int c, float *h) {
-    Vec<T> t;
-    load_x<T, Move::kCached>(A.x, A.x_stride, at, c, dim - c, t);
+  for (int64_t i = blockIdx.x; i < A.rows; i += gridDim.x) {
+    const int64_t at = Source{A.ids, A.x_rows}.at(i);
+    auto load_h = [&](int c, float *h) {
+      Vec<T> t;
+      load_x<T, Move::kCached>(A.x, A.x_stride, at, c, dim - c, t);
 #pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = float(t.e[j]);
-    if (A.residual) {
-      t.load(static_cast<const T *>(A.residual) + i * A.residual_stride + c, dim - c);
+      for (int j = 0; j < V; ++j) h[j] = float(t.e[j]);
+      if (A.residual) {
+        t.load(static_cast<const T *>(A.residual) + i * A.residual_stride + c, dim - c);
 #pragma unroll
-      for (int j = 0; j < V; ++j) h[j] += float(t.e[j]);
-    }
-  };
-  float ss = 0.0f;
-  for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
-    float h[V];
-    load_h(c, h);
-#pragma unroll
-    for (int j = 0; j < V; ++j) ss += h[j] * h[j];
-  }
-  const float s = rsqrtf(grp.sum(ss) / float(dim) + A.eps);
-  float f = 1.0f;
-  if (E4M3) {
-    uint32_t amax = 0;
+        for (int j = 0; j < V; ++j) h[j] += float(t.e[j]);
+      }
+    };
+    float ss = 0.0f;
     for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      float h[V];
+      load_h(c, h);
+#pragma unroll
+      for (int j = 0; j < V; ++j) ss += h[j] * h[j];
+    }
+    const float s = rsqrtf(grp.sum(ss) / float(dim) + A.eps);
+    float f = 1.0f;
+    if (E4M3) {
+      uint32_t amax = 0;
+      for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+        float h[V], w[V];
+        load_h(c, h);
+        load_weight<T>(A, c, dim - c, w);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (j < dim - c) amax = max(amax, mag(h[j] * s * w[j]));
+      }
+      const float sc = scale_of(grp.max(amax));
+      f = 1.0f / sc;
+      if (threadIdx.x == 0) A.scale[i] = sc;
+    }
+    // (a lane reads what it overwrites before it does, and no other lane's)
+    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      const int n = dim - c;
       float h[V], w[V];
       load_h(c, h);
-      load_weight<T>(A, c, dim - c, w);
+      load_weight<T>(A, c, n, w);
+      if (A.sum) store_row<T>(static_cast<T *>(A.sum) + i * A.sum_stride + c, h, n);
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j < dim - c) amax = max(amax, mag(h[j] * s * w[j]));
+      for (int j = 0; j < V; ++j) h[j] = h[j] * s * w[j] * f;
+      if (E4M3)
+        store_e4m3<V>(static_cast<uint8_t *>(A.y) + i * A.y_stride + c, h, n);
+      else
+        store_row<T>(static_cast<T *>(A.y) + i * A.y_stride + c, h, n);
     }
-    const float sc = scale_of(grp.max(amax));
-    f = 1.0f / sc;
-    if (threadIdx.x == 0) A.scale[i] = sc;
-  }
-  // (a lane reads what it overwrites before it does, and no other lane's)
-  for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
-    const int n = dim - c;
-    float h[V], w[V];
-    load_h(c, h);
-    load_weight<T>(A, c, n, w);
-    if (A.sum) store_row<T>(static_cast<T *>(A.sum) + i * A.sum_stride + c, h, n);
-#pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = h[j] * s * w[j] * f;
-    if (E4M3)
-      store_e4m3<V>(static_cast<uint8_t *>(A.y) + i * A.y_stride + c, h, n);
-    else
-      store_row<T>(static_cast<T *>(A.y) + i * A.y_stride + c, h, n);
   }
 }
 
@@ -534,8 +535,9 @@ struct Forward {
   hipError_t run() const {
     const int64_t blocks = ceil_div<int64_t>(A.rows, Group<G>::kRows);
     if constexpr (NV == 0) {
-      hipLaunchKernelGGL((k_rms_norm_long<T, E4M3>), dim3(unsigned(blocks)), dim3(kBlock), 0,
-                         stream, A);
+      hipLaunchKernelGGL((k_rms_norm_long<T, E4M3>),
+                         dim3(unsigned(blocks < 65536 ? blocks : 65536)), dim3(kBlock), 0, stream,
+                         A);
     } else {
       hipLaunchKernelGGL((k_rms_norm<T, G, NV, E4M3>),
                          dim3(unsigned(blocks < kResident ? blocks : kResident)), dim3(kBlock), 0,

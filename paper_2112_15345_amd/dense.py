@@ -4,7 +4,8 @@ forward and backward.
 
 Argument marshalling only, in the native module.  Matrices are 2-D tensors; rows may have any stride, and
 a tensor whose columns are not contiguous is copied first.  Outputs and workspaces
-are made on `stream` (default: the current stream), where the work runs.
+are made on `stream` (default: the current stream), where the work runs; as with any
+torch call, tensors made on another stream have to be ready, and kept until it is done.
 
     y, h, scale = rms_norm(x, weight, residual=r)            # h = x + r
     z, pre = linear(y, w, bias=b, act="gelu", residual=h, keep_pre=True)
@@ -88,6 +89,9 @@ def _call(name, stream, *args):
     if stream is None:
         r = f(*args)
     else:
+        for a in args:
+            if isinstance(a, torch.Tensor) and a.device != stream.device:
+                raise ValueError(f"a tensor on {a.device} and a stream of {stream.device}")
         with torch.cuda.stream(stream):
             r = f(*args)
     if type(r) is int:
