@@ -76,16 +76,21 @@ COUNTER_TRAFFIC = [
 ]
 
 
+DENSE_SOURCES = ("hg_dense.cpp", "hg_dense.hpp", "hg_dense_py.cpp", "hg_distill.hip",
+                 "hg_linear.hip", "hg_norm.hip")
+
+
 def kernel_sources_digest():
-    """A digest of the kernel and runtime sources' code: comments and
-    whitespace are left out, so that editing a comment keeps measured
-    counters valid while any change to the code drops them."""
+    """A digest of the mini-batch path's kernel and runtime sources' code:
+    comments and whitespace are left out, so that editing a comment keeps
+    measured counters valid while any change to the code drops them.  (The
+    dense operators' sources share no kernel with the path.)"""
     import hashlib
     import re
     d = os.path.join(ROOT, "paper_2112_15345_amd", "csrc")
     h = hashlib.sha256()
     for f in sorted(os.listdir(d)):
-        if f.endswith((".hip", ".hpp", ".cpp")):
+        if f.endswith((".hip", ".hpp", ".cpp")) and f not in DENSE_SOURCES:
             text = open(os.path.join(d, f), encoding="utf-8").read()
             text = re.sub(r"/\*.*?\*/", " ", text, flags=re.S)
             text = re.sub(r"//[^\n]*", " ", text)

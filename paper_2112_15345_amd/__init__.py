@@ -4,8 +4,8 @@ generation on MI355X (DistDGLv2, arXiv 2112.15345, Sec. 3.2 and Sec. 4.2).
 Argument marshalling only: every step of the path runs in the library's gfx950
 kernels.  PyTorch supplies device memory (the graph, feature tables, outputs)
 and the stream (the current torch stream).  The tensors over a mini-batch's
-arrays are made by the native module _hgviews, built for one version of Python
-and PyTorch.  Import fails loudly if either
+arrays are made by the native module _hgviews (the dense operators' by _hgdense),
+built for one version of Python and PyTorch.  Import fails loudly if one of them
 is not built; there is no CPU path.
 
     g = Graph(ntypes=[(num_nodes, feat_or_None), ...],
@@ -34,6 +34,8 @@ LIB_PATH = os.path.join(_HERE, "libhg.so")
 # compiled against PyTorch's C++ headers: the name says which PyTorch's
 VIEWS_PATH = os.path.join(
     _HERE, f"_hgviews.{sys.implementation.cache_tag}.torch-{torch.__version__}.so")
+DENSE_PATH = os.path.join(
+    _HERE, f"_hgdense.{sys.implementation.cache_tag}.torch-{torch.__version__}.so")
 
 HG_OK, HG_EINVAL, HG_ENOMEM, HG_EDEVICE, HG_EUNSUPPORTED = 0, -1, -2, -3, -4
 HG_DT_NONE, HG_DT_F32, HG_DT_F16, HG_DT_BF16 = 0, 1, 2, 3
@@ -180,28 +182,35 @@ def _accessors(lib: ctypes.CDLL):
 
 _lib = None
 _views = None
+_dense = None
+
+
+def _load_module(name: str, path: str):
+    spec = importlib.util.spec_from_file_location(f"{__name__}.{name}", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
-    """Loads libhg.so and the binding's native module; raises if either has not
-    been built (no fallback path)."""
-    global _lib, _views
+    """Loads libhg.so and the binding's native modules; raises if one has not been
+    built (no fallback path)."""
+    global _lib, _views, _dense
     if _lib is None:
-        for need in (path, VIEWS_PATH):
+        for need in (path, VIEWS_PATH, DENSE_PATH):
             if not os.path.exists(need):
                 raise ImportError(f"{need} is missing: build it (again for another "
                                   "Python or PyTorch) with "
                                   "`python -m paper_2112_15345_amd.build`")
         lib = _bind(ctypes.CDLL(path))
-        spec = importlib.util.spec_from_file_location(f"{__name__}._hgviews", VIEWS_PATH)
-        views = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(views)
+        views = _load_module("_hgviews", VIEWS_PATH)
         views.bind(*_accessors(lib))
-        views.bind_dense(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        dense = _load_module("_hgdense", DENSE_PATH)
+        dense.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.hg_rms_norm, lib.hg_rms_norm_grad, lib.hg_rms_norm_grad_workspace, lib.hg_linear,
             lib.hg_linear_workspace, lib.hg_linear_grad, lib.hg_linear_grad_workspace,
             lib.hg_distill)))
-        _views = views
+        _views, _dense = views, dense
         _lib = lib
     return _lib
 

@@ -1,9 +1,9 @@
 """Builds libhg.so (the gfx950 kernels and the C ABI of include/hg.h) and the
-Python binding's native module _hgviews in-tree.
+Python binding's native modules _hgviews and _hgdense in-tree.
 
 Every source of the library is compiled with hipcc for gfx950 only, then linked
-into one shared library next to this file; _hgviews is host code against the
-installed PyTorch, whose version its file name has.  `python -m paper_2112_15345_amd.build` runs it.
+into one shared library next to this file; the modules are host code against the
+installed PyTorch, whose version their file names have.  `python -m paper_2112_15345_amd.build` runs it.
 """
 from __future__ import annotations
 
@@ -51,37 +51,38 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
-def _build_views(verbose: bool) -> None:
-    """Compiles and links _hgviews (host code only)."""
+def _build_views(source: str, target: str, verbose: bool, *libs: str) -> None:
+    """Compiles and links one of the binding's native modules (host code only)."""
     import torch
-    from . import VIEWS_PATH
     import torch.utils.cpp_extension as ext
     libdir = os.path.join(os.path.dirname(torch.__file__), "lib")
-    tmp = VIEWS_PATH + ".tmp"
+    tmp = target + ".tmp"
     inc = [x for p in (*ext.include_paths(), sysconfig.get_paths()["include"], "/opt/rocm/include")
            for x in ("-isystem", p)]
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-D__HIP_PLATFORM_AMD__=1", "-I", INCLUDE, *inc,
-           os.path.join(CSRC, "hg_views.cpp"), os.path.join(CSRC, "hg_dense_py.cpp"), "-o", tmp,
-           "-L", libdir, "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip", "-ltorch_python",
-           f"-Wl,-rpath,{libdir}"]
+           os.path.join(CSRC, source), "-o", tmp, "-L", libdir, "-ltorch", "-ltorch_cpu",
+           "-lc10", *libs, "-ltorch_python", f"-Wl,-rpath,{libdir}"]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError(f"g++ failed on hg_views.cpp, hg_dense_py.cpp:\n{res.stdout}\n{res.stderr}")
-    os.replace(tmp, VIEWS_PATH)
+        raise RuntimeError(f"g++ failed on {source}:\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, target)
 
 
 def build(verbose: bool = False) -> str:
     """Compiles every source for gfx950 and links libhg.so (returns its path), and
-    builds _hgviews."""
+    builds _hgviews and _hgdense."""
+    from . import DENSE_PATH, VIEWS_PATH
     os.makedirs(OBJDIR, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        views = ex.submit(_build_views, verbose)
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 2) as ex:
+        views = [ex.submit(_build_views, "hg_views.cpp", VIEWS_PATH, verbose),
+                 ex.submit(_build_views, "hg_dense_py.cpp", DENSE_PATH, verbose, "-lc10_hip")]
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-        views.result()
+        for v in views:
+            v.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     if verbose:

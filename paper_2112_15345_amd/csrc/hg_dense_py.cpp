@@ -1,4 +1,4 @@
-// The dense operators for the Python binding (part of module _hgviews): tensors checked,
+// The dense operators for the Python binding (module _hgdense): tensors checked,
 // outputs and workspaces made, and the library's entry point called in one native call.
 // A call on one row takes some 5 us on the device; through ctypes structures and torch's
 // Python functions its marshalling took 12 to 15.
@@ -177,7 +177,7 @@ PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F f) {
     return nullptr;
   }
   if (!api.distill) {
-    PyErr_SetString(PyExc_RuntimeError, "bind_dense() has not been called");
+    PyErr_SetString(PyExc_RuntimeError, "bind() has not been called");
     return nullptr;
   }
   try {
@@ -443,10 +443,10 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
-// bind_dense(addresses of the entry points, in Api's order)
-PyObject *bind_dense(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// bind(addresses of the entry points, in Api's order)
+PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (n != 8) {
-    PyErr_SetString(PyExc_TypeError, "bind_dense() takes eight addresses");
+    PyErr_SetString(PyExc_TypeError, "bind() takes eight addresses");
     return nullptr;
   }
   int64_t v[8];
@@ -471,12 +471,17 @@ PyMethodDef method(const char *name) {
           nullptr};
 }
 
+PyMethodDef methods[] = {method<bind>("bind"),
+                         method<rms_norm>("rms_norm"),
+                         method<rms_norm_grad>("rms_norm_grad"),
+                         method<linear>("linear"),
+                         method<linear_grad>("linear_grad"),
+                         method<distill>("distill"),
+                         {nullptr, nullptr, 0, nullptr}};
+
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hgdense", nullptr, -1, methods,
+                      nullptr, nullptr, nullptr, nullptr};
+
 }  // namespace
 
-PyMethodDef hg_dense_methods[] = {method<bind_dense>("bind_dense"),
-                                  method<rms_norm>("rms_norm"),
-                                  method<rms_norm_grad>("rms_norm_grad"),
-                                  method<linear>("linear"),
-                                  method<linear_grad>("linear_grad"),
-                                  method<distill>("distill"),
-                                  {nullptr, nullptr, 0, nullptr}};
+PyMODINIT_FUNC PyInit__hgdense(void) { return PyModule_Create(&module); }

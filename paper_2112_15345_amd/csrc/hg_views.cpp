@@ -9,7 +9,6 @@
 // which every returned tensor keeps alive) and the wanted device index (-1:
 // where the array is).  A failed accessor's status is returned as an int; the
 // accessors are those of the library that the binding has loaded (bind()).
-// The module's other half, the dense operators, is in hg_dense_py.cpp.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -247,13 +246,4 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hgviews", nullptr, -1, methods,
 
 }  // namespace
 
-extern PyMethodDef hg_dense_methods[];  // hg_dense_py.cpp
-
-PyMODINIT_FUNC PyInit__hgviews(void) {
-  PyObject *m = PyModule_Create(&module);
-  if (m && PyModule_AddFunctions(m, hg_dense_methods) != 0) {
-    Py_DECREF(m);
-    return nullptr;
-  }
-  return m;
-}
+PyMODINIT_FUNC PyInit__hgviews(void) { return PyModule_Create(&module); }

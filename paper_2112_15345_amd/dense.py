@@ -74,13 +74,13 @@ _native = None
 
 
 def _module():
-    """The native module's dense half (csrc/hg_dense_py.cpp), which checks the tensors, makes
-    the outputs and calls the library."""
+    """The native module _hgdense (csrc/hg_dense_py.cpp), which checks the tensors, makes the
+    outputs and calls the library."""
     global _native
     if _native is None:
         load_library()
-        from . import _views
-        _native = _views
+        from . import _dense
+        _native = _dense
     return _native
 
 
