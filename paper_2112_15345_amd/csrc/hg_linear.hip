@@ -192,6 +192,7 @@ struct Operand {
   const void *p;
   int64_t stride;  // elements between stored rows
   int64_t rows;    // extent along C's axis
+  bool padded = false;  // rows of whole 16-byte pieces, the last one's rest zeros
 };
 
 // Where the 16-byte piece c of stored row r of an operand's slab lies in LDS
@@ -902,19 +903,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
 
 constexpr int kSumRows = 64;  // rows of C that one part of the column sums covers
 
-// dz = dy act'(pre) in T (dz NULL: not written), and the sums over the block's rows.
+// dz = dy act'(pre) in T (dz NULL: not written), zeros from column n to its stride, and the
+// sums over the block's rows.
 // A wavefront takes 64 vectors of 8 columns; the block's four take turns over the rows.
 // Block b: columns b % strips, rows b / strips.
 template <typename T>
 __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, const T *pre,
                                             int64_t pre_stride, int32_t act, int64_t m, int64_t n,
-                                            int64_t strips, T *dz, float *part) {
+                                            int64_t strips, T *dz, int64_t dz_stride, float *part) {
   __shared__ float red[4][64 * 8 + 8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t strip = blockIdx.x % strips, chunk = blockIdx.x / strips;
   const int64_t j = (strip * 64 + lane) * 8;
   const int64_t r0 = chunk * kSumRows, r1 = min(m, r0 + kSumRows);
-  const int left = int(min<int64_t>(8, n - j));
+  const int left = int(min<int64_t>(8, n - j)), wide = int(min<int64_t>(8, dz_stride - j));
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   constexpr int U = 4;  // rows in flight
   if (left > 0)
@@ -939,7 +941,11 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, cons
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[k] *= act_slope<decltype(a)::value>(float(z[u].e[k]));
         });
-        if (dz) put<T, 8>(dz, i * n + j, v, left);
+        if (left < 8) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = k < left ? v[k] : 0.0f;
+        }
+        if (dz) put<T, 8>(dz, i * dz_stride + j, v, wide);
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] += v[k];
       }
@@ -952,6 +958,26 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, cons
     const int64_t col = strip * 512 + c;
     if (col < n)
       part[chunk * n + col] = red[0][c] + red[1][c] + red[2][c] + red[3][c];
+  }
+}
+
+// ---- operands laid out anew ---------------------------------------------------------
+
+// Rows of `cols` elements into rows of per_row 16-byte pieces, the last one's rest zeros.
+template <typename S>
+__global__ __launch_bounds__(256) void k_lay(const S *from, int64_t stride, int64_t cols,
+                                             uint32_t per_row, uint32_t pieces, u32x4 *to) {
+  u32x4 v[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const uint32_t t = blockIdx.x * 1024 + u * 256 + threadIdx.x;
+    const int64_t row = t / per_row, c = int64_t(t % per_row) * (16 / int(sizeof(S)));
+    if (t < pieces) v[u] = row_piece(from + row * stride, c, cols);
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const uint32_t t = blockIdx.x * 1024 + u * 256 + threadIdx.x;
+    if (t < pieces) to[t] = v[u];
   }
 }
 
@@ -1008,13 +1034,23 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both)
     const int64_t tiles = tiles_of(rows, cols, p.tile_i, p.tile_j);
     if (tiles < at_once) {
       // the depth in parts of at least 8 slabs; where half the blocks are there anyway, only
-      // a depth that is long next to the writing and adding of the parts
+      // a depth that is long next to the writing and adding of the parts: as many that their
+      // rounds take least, a part's writing and adding taken as 1/32 of a slab (5408 x 912
+      // over 26506 rows in float32, 344 tiles: 1825 us as 4 parts each, 2354 as one)
+      const bool most_there = 2 * tiles >= at_once;
       const int64_t long_ = p.cut == Cut::kSmall ? 16 * slab : 64 * slab;
-      const int64_t least = 2 * tiles >= at_once ? long_ : 8 * slab;
-      const int64_t want = at_once / tiles, most = depth / least;
-      p.splits = want < most ? want : most;
-      if (p.splits > 256) p.splits = 256;
-      if (p.splits < 1) p.splits = 1;
+      const int64_t most = depth / (most_there ? long_ : 8 * slab);
+      if (most_there) {
+        double least = 0.0;
+        for (int64_t s = 1; s <= std::min<int64_t>(8, most); ++s) {
+          const double t = double(ceil_div<int64_t>(tiles * s, at_once)) * double(depth) /
+                               double(s * slab) + (s > 1 ? 8.0 + double(s * tiles) / 32.0 : 0.0);
+          if (s == 1 || t < least) p.splits = s, least = t;
+        }
+      } else {
+        const int64_t want = std::min<int64_t>(at_once / tiles, 256);
+        p.splits = std::max<int64_t>(1, std::min(want, most));
+      }
     } else if (tiles <= 6 * at_once && filled(tiles, at_once) < 0.9 && depth >= 16 * slab) {
       // the rows of whole rounds; the last round's few tiles would leave most units idle
       // for as long as a full one takes, and are cut finer
@@ -1039,12 +1075,43 @@ int64_t parts_bytes(int64_t rows, int64_t cols, int64_t depth, int64_t slab, boo
   return most;
 }
 
-// Whether every 16-byte piece of an operand is aligned, and lies in it or outside it.
+// Whether every 16-byte piece of an operand is aligned, and lies in it or outside it, or
+// ends in zeros.
 template <typename S>
 bool is_direct(const Operand &O, bool turned, int64_t depth) {
   constexpr int64_t E = 16 / int64_t(sizeof(S));
   return reinterpret_cast<uintptr_t>(O.p) % 16 == 0 && O.stride % E == 0 &&
-         (turned ? O.rows : depth) % E == 0;
+         (O.padded || (turned ? O.rows : depth) % E == 0);
+}
+
+// The elements of a row laid out in whole pieces.
+int64_t padded(int64_t cols, int64_t size) { return align16(cols * size) / size; }
+
+// Whether a product's operands whose rows are not whole 16-byte pieces are first copied
+// into rows that are, for the kernel of aligned operands: where the product is large and
+// every element is used often enough (us, forward / dx / dw, without and with the copies):
+//   bfloat16  13222 x 2594 x 3968  401 / 630 / 865, 335 / 325 / 359
+//              4096 x  255 x 4097   41 / 128 /  82,  41 /  64 /  68
+//             16385 x  515 x  515   29 /  45 /  95,  45 /  50 /  69
+//              1000 x 1001 x 1003   15 /  21 /  30,  20 /  34 /  35
+//   float32   13222 x 2594 x 3968  2363 / 2669 / 2969, 1708 / 1660 / 1719
+//              1000 x 1001 x 1003   37 /  47 /  51,  42 /  52 /  52
+// (Operands of 16 GiB and more are not copied.)
+bool is_laid(int64_t m, int64_t k, int64_t n, int64_t size) {
+  return std::min(m, std::min(k, n)) >= 250 && double(m) * double(k) * double(n) >= 4e9 &&
+         double(std::max(m, n)) * double(padded(k, size) * size) < 1.6e10;
+}
+// Copies an operand of rows x cols to `to`.
+template <typename S>
+hipError_t lay(Operand &O, int64_t rows, int64_t cols, bool turned, char *to, hipStream_t stream) {
+  const int64_t stride = padded(cols, sizeof(S));
+  const uint32_t per_row = uint32_t(stride * sizeof(S) / 16);
+  const int64_t n = rows * per_row;  // (below 2^30)
+  hipLaunchKernelGGL((k_lay<S>), dim3(unsigned(ceil_div<int64_t>(n, 1024))), dim3(256), 0, stream,
+                     static_cast<const S *>(O.p), O.stride, cols, per_row, uint32_t(n),
+                     reinterpret_cast<u32x4 *>(to));
+  O = Operand{to, stride, turned ? stride : rows, true};
+  return hipGetLastError();
 }
 
 template <typename S, bool TP, bool TQ, int BI, int BJ, int kWavesI, int kWavesJ, int W,
@@ -1097,11 +1164,11 @@ hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The operand, and the epilogue, of n rows of C from row `at` on.
+// The operand of the rows of C from row `at` on, and the epilogue of n of them.
 template <typename S>
-Operand rows_from(Operand Q, bool turned, int64_t at, int64_t n) {
+Operand rows_from(Operand Q, bool turned, int64_t at) {
   Q.p = static_cast<const S *>(Q.p) + (turned ? at : at * Q.stride);
-  Q.rows = n;
+  Q.rows -= at;
   return Q;
 }
 Epilogue epilogue_from(Epilogue E, int64_t at, int64_t n) {
@@ -1143,7 +1210,7 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
     // (any operands: tiles of 128 x 128 or 64 x 64; the parts and rows stay as planned)
     if (!direct && p.cut != Cut::kSmall) p.cut = Cut::kMedium, p.tile_i = p.tile_j = 128;
     Product B = A;
-    B.Q = rows_from<S>(Q, TQ, done, p.rows);
+    B.Q = rows_from<S>(Q, TQ, done);
     B.E = epilogue_from(E, done, p.rows);
     const int64_t ti = ceil_div<int64_t>(p.rows, p.tile_i), tj = ceil_div<int64_t>(E.cols, p.tile_j);
     if (ti * tj * 512 >= int64_t(1) << 32) return hipErrorInvalidConfiguration;  // threads of a grid
@@ -1174,6 +1241,27 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
   return hipSuccess;
 }
 
+struct LinearSpace {  // byte offsets in the workspace
+  int64_t w, x, parts, total;
+  bool laid;
+};
+LinearSpace linear_space(int64_t m, int64_t k, int64_t n, int32_t dtype) {
+  LinearSpace s{0, 0, 0, 0, false};
+  if (is_few(m, n)) {
+    const int64_t splits = few_plan(n, k, size_of(dtype)).splits;
+    s.total = splits > 1 ? splits * m * n * 4 : 0;
+    return s;
+  }
+  const int64_t size = size_of(dtype), row = padded(k, size);
+  s.laid = row != k && is_laid(m, k, n, size);
+  if (s.laid) {
+    s.x = n * row * size;
+    s.parts = s.x + m * row * size;
+  }
+  s.total = s.parts + parts_bytes(m, n, k, slab_of(dtype), false);
+  return s;
+}
+
 template <typename T>
 hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
   Epilogue E{};
@@ -1193,19 +1281,34 @@ hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
     E.row_scale = A.x_scale;
     E.col_scale = A.w_scale;
   }
-  return product<T, false, false>(Operand{A.w, A.w_stride, A.n}, Operand{A.x, A.x_stride, A.m},
-                                  A.k, E, static_cast<float *>(A.workspace), stream);
+  Operand w{A.w, A.w_stride, A.n}, x{A.x, A.x_stride, A.m};
+  const LinearSpace s = linear_space(A.m, A.k, A.n, A.dtype);
+  char *const ws = static_cast<char *>(A.workspace);
+  if (s.laid) {
+    hipError_t e = lay<T>(w, A.n, A.k, false, ws + s.w, stream);
+    if (e == hipSuccess) e = lay<T>(x, A.m, A.k, false, ws + s.x, stream);
+    if (e != hipSuccess) return e;
+  }
+  return product<T, false, false>(w, x, A.k, E, reinterpret_cast<float *>(ws + s.parts), stream);
 }
 
 struct GradSpace {  // byte offsets in the workspace
-  int64_t dz, sums, parts, total;
+  int64_t dz, sums, x, w, parts, total;
+  int64_t dz_stride;  // of dz in the workspace
+  bool dz_laid, laid;
 };
 GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
   GradSpace g;
   const int64_t slab = slab_of(dtype);
+  const int64_t size = size_of(dtype), row = padded(k, size);
   g.dz = 0;
-  g.sums = align16(act == HG_ACT_NONE ? 0 : m * n * size_of(dtype));
-  g.parts = g.sums + align16(ceil_div<int64_t>(m, kSumRows) * n * 4);
+  g.dz_stride = padded(n, size);
+  g.laid = row != k && is_laid(m, k, n, size);
+  g.dz_laid = act != HG_ACT_NONE || (g.dz_stride != n && is_laid(m, k, n, size));
+  g.sums = g.dz_laid ? m * g.dz_stride * size : 0;
+  g.x = g.sums + align16(ceil_div<int64_t>(m, kSumRows) * n * 4);
+  g.w = g.x + (g.laid ? m * row * size : 0);
+  g.parts = g.w + (g.laid ? n * row * size : 0);
   const int64_t a = parts_bytes(m, k, n, slab, false), b = parts_bytes(n, k, m, slab, true);
   g.total = g.parts + align16(a > b ? a : b);
   return g;
@@ -1215,25 +1318,24 @@ template <typename T>
 hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
   const GradSpace g = grad_space(A.m, A.k, A.n, A.dtype, A.act);
   char *const ws = static_cast<char *>(A.workspace);
-  const T *dz = static_cast<const T *>(A.dy);
-  int64_t dz_stride = A.dy_stride;
+  Operand dz{A.dy, A.dy_stride, A.m}, dz_turned{A.dy, A.dy_stride, A.n};
   const bool has_act = A.act != HG_ACT_NONE;
   const int64_t chunks = ceil_div<int64_t>(A.m, kSumRows);
   const bool products = (A.dx || A.dw) && A.k > 0;
-  if (A.m > 0 && A.n > 0 && ((has_act && products) || A.dbias)) {
+  if (A.m > 0 && A.n > 0 && ((g.dz_laid && products) || A.dbias)) {
     const int64_t strips = ceil_div<int64_t>(A.n, 512);
     if (strips * chunks * 256 >= int64_t(1) << 32) return hipErrorInvalidConfiguration;
-    T *const to = has_act && products ? reinterpret_cast<T *>(ws + g.dz) : nullptr;
+    T *const to = g.dz_laid && products ? reinterpret_cast<T *>(ws + g.dz) : nullptr;
     float *const sums = A.dbias ? reinterpret_cast<float *>(ws + g.sums) : nullptr;
     hipLaunchKernelGGL((k_dz<T>), dim3(unsigned(strips * chunks)), dim3(256), 0, stream,
                        static_cast<const T *>(A.dy), A.dy_stride,
                        has_act ? static_cast<const T *>(A.pre) : nullptr, A.pre_stride, A.act, A.m,
-                       A.n, strips, to, sums);
+                       A.n, strips, to, g.dz_stride, sums);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (to) {
-      dz = to;
-      dz_stride = A.n;
+      dz = Operand{to, g.dz_stride, A.m, true};
+      dz_turned = Operand{to, g.dz_stride, g.dz_stride, true};
     }
   }
   if (A.dbias) {
@@ -1249,8 +1351,9 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
     E.rows = A.m;
     E.cols = A.k;
     E.dtype = A.dtype;
-    hipError_t e = product<T, true, false>(Operand{A.w, A.w_stride, A.k},
-                                           Operand{dz, dz_stride, A.m}, A.n, E, parts, stream);
+    Operand w{A.w, A.w_stride, A.k};
+    hipError_t e = g.laid ? lay<T>(w, A.n, A.k, true, ws + g.w, stream) : hipSuccess;
+    if (e == hipSuccess) e = product<T, true, false>(w, dz, A.n, E, parts, stream);
     if (e != hipSuccess) return e;
   }
   if (A.dw) {
@@ -1260,8 +1363,9 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
     E.rows = A.n;
     E.cols = A.k;
     E.dtype = A.dw_dtype;
-    return product<T, true, true>(Operand{A.x, A.x_stride, A.k}, Operand{dz, dz_stride, A.n}, A.m,
-                                  E, parts, stream);
+    Operand x{A.x, A.x_stride, A.k};
+    hipError_t e = g.laid ? lay<T>(x, A.m, A.k, true, ws + g.x, stream) : hipSuccess;
+    return e != hipSuccess ? e : product<T, true, true>(x, dz_turned, A.m, E, parts, stream);
   }
   return hipSuccess;
 }
@@ -1269,11 +1373,7 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
 }  // namespace
 
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {
-  if (is_few(m, n)) {
-    const int64_t splits = few_plan(n, k, size_of(dtype)).splits;
-    return splits > 1 ? splits * m * n * 4 : 0;
-  }
-  return parts_bytes(m, n, k, slab_of(dtype), false);
+  return linear_space(m, k, n, dtype).total;
 }
 
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream) {
