@@ -377,53 +377,54 @@ __device__ __forceinline__ void get_as(const void *base, int32_t dtype, int64_t 
     get<__bf16, N>(base, at, v, n);
 }
 
-// 8 columns of C, from j on, n of them in C: what is the same for every row.
+// N columns of C, from j on, n of them in C: what is the same for every row.
+template <int N>
 struct Columns {
   int64_t j;
   int n;
-  float bias[8], scale[8];
+  float bias[N], scale[N];
   __device__ __forceinline__ Columns(const Epilogue &E, int64_t at) : j(at) {
-    n = int(max<int64_t>(0, min<int64_t>(8, E.cols - j)));
+    n = int(max<int64_t>(0, min<int64_t>(N, E.cols - j)));
 #pragma unroll
-    for (int k = 0; k < 8; ++k) bias[k] = 0.0f, scale[k] = 1.0f;
+    for (int k = 0; k < N; ++k) bias[k] = 0.0f, scale[k] = 1.0f;
     if (n > 0 && !E.part) {
-      if (E.bias) get_as<8>(E.bias, E.bias_dtype, j, bias, n);
-      if (E.col_scale) get<float, 8>(E.col_scale, j, scale, n);
+      if (E.bias) get_as<N>(E.bias, E.bias_dtype, j, bias, n);
+      if (E.col_scale) get<float, N>(E.col_scale, j, scale, n);
     }
   }
 };
 
 // The columns' sums v of row i, to the result (n > 0; O: its type); `residual`: the row's.
-template <typename O, bool kPlain>
-__device__ __forceinline__ void finish(const Epilogue &E, const Columns &C, int64_t i,
-                                       const Vec<O, 8> &residual, float *v) {
+template <typename O, bool kPlain, int N>
+__device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, int64_t i,
+                                       const Vec<O, N> &residual, float *v) {
   if (kPlain) {
-    put<O, 8, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
+    put<O, N, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
     return;
   }
   if (E.col_scale) {
     const float r = E.row_scale[i];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= r * C.scale[k];
+    for (int k = 0; k < N; ++k) v[k] *= r * C.scale[k];
   }
   if (E.bias) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += C.bias[k];
+    for (int k = 0; k < N; ++k) v[k] += C.bias[k];
   }
-  if (E.pre) put<O, 8, Move::kStreamed>(E.pre, i * E.pre_stride + C.j, v, C.n);
+  if (E.pre) put<O, N, Move::kStreamed>(E.pre, i * E.pre_stride + C.j, v, C.n);
   with_act(E.act, [&](auto act) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = act_of<decltype(act)::value>(v[k]);
+    for (int k = 0; k < N; ++k) v[k] = act_of<decltype(act)::value>(v[k]);
   });
   if (E.residual) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += float(residual.e[k]);
+    for (int k = 0; k < N; ++k) v[k] += float(residual.e[k]);
   }
-  put<O, 8, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
+  put<O, N, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
 }
-template <typename O>
-__device__ __forceinline__ void load_residual(const Epilogue &E, const Columns &C, int64_t i,
-                                              Vec<O, 8> &r) {
+template <typename O, int N>
+__device__ __forceinline__ void load_residual(const Epilogue &E, const Columns<N> &C, int64_t i,
+                                              Vec<O, N> &r) {
   if (E.residual)
     r.template load<Move::kStreamed>(static_cast<const O *>(E.residual) + i * E.residual_stride + C.j, C.n);
 }
@@ -462,44 +463,53 @@ __device__ __forceinline__ void tile_of(const Product &A, int64_t b, int64_t &ti
   tj = t / high;
 }
 
-// The waves' parts of C through LDS, 16 rows at a time: a lane's 4 neighbours in, 8
-// neighbours out, so that whole rows of the part are read and written together.  A lane
-// keeps its columns; the residual is loaded 16 rows ahead.
+// The waves' parts of C through LDS, 16 rows at a time: a lane's 4 neighbours in, 16 bytes
+// of neighbours out (N of them), so that a store's lanes write whole rows of the part: with
+// 8 neighbours in 32 bits, two stores to a lane's 32 bytes, the halves of lines went out by
+// themselves (the gradient of 4096 x 4096 weights over 8 rows: 36 us, now 20).  A lane keeps its columns; the residual
+// is loaded 16 rows ahead.
 // kPlain: nothing but the sums (the gradients).
+template <int N, int NJ>
+struct Out {
+  static constexpr int WJ = NJ * 16;
+  static constexpr int LD = WJ + 4;  // floats; the 4 spread the rows over the banks
+  static constexpr int kAcross = WJ / N, kDown = 64 / kAcross;  // lanes of a row, rows at a time
+  static constexpr int U = 16 / kDown;
+  float *const out;
+  const int lane, r, c;
+  __device__ __forceinline__ explicit Out(char *lds)
+      : out(reinterpret_cast<float *>(lds) + (threadIdx.x >> 6) * 16 * LD),
+        lane(threadIdx.x & 63), r(lane / kAcross), c(lane % kAcross * N) {}
+  __device__ __forceinline__ void exchange(const f32x4 (&acc)[NJ]) const {
+#pragma unroll
+    for (int b = 0; b < NJ; ++b)
+      *reinterpret_cast<f32x4 *>(out + (lane & 15) * LD + 16 * b + 4 * (lane >> 4)) = acc[b];
+    wave_sync();
+  }
+  __device__ __forceinline__ void take(int u, float *v) const {
+#pragma unroll
+    for (int h = 0; h < N; h += 4)
+      *reinterpret_cast<f32x4 *>(v + h) =
+          *reinterpret_cast<const f32x4 *>(out + (u * kDown + r) * LD + c + h);
+  }
+};
 template <bool kPlain, int NI, int NJ>
 __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i0, int64_t j0,
                                           const f32x4 (&acc)[NI][NJ]) {
-  constexpr int WJ = NJ * 16;
-  constexpr int LD = WJ + 4;  // floats; the 4 spread the rows over the banks
-  constexpr int kAcross = WJ / 8, kDown = 64 / kAcross;  // lanes of a row, rows at a time
-  constexpr int U = 16 / kDown;
   const Epilogue &E = A.E;
-  const int lane = threadIdx.x & 63;
-  float *const out = reinterpret_cast<float *>(lds) + (threadIdx.x >> 6) * 16 * LD;
-  const int r = lane / kAcross, c = lane % kAcross * 8;
-  const Columns C(E, j0 + c);
-  const auto exchange = [&](int a) {
-#pragma unroll
-    for (int b = 0; b < NJ; ++b)
-      *reinterpret_cast<f32x4 *>(out + (lane & 15) * LD + 16 * b + 4 * (lane >> 4)) = acc[a][b];
-    wave_sync();
-  };
-  const auto take = [&](int u, float *v) {
-    const float *const p = out + (u * kDown + r) * LD + c;
-    *reinterpret_cast<f32x4 *>(v) = *reinterpret_cast<const f32x4 *>(p);
-    *reinterpret_cast<f32x4 *>(v + 4) = *reinterpret_cast<const f32x4 *>(p + 4);
-  };
   if (E.part) {
+    const Out<4, NJ> L(lds);
+    const Columns<4> C(E, j0 + L.c);
 #pragma unroll
     for (int a = 0; a < NI; ++a) {
-      exchange(a);
+      L.exchange(acc[a]);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = i0 + 16 * a + u * kDown + r;
-        float v[8];
-        take(u, v);
+      for (int u = 0; u < L.U; ++u) {
+        const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
+        float v[4];
+        L.take(u, v);
         if (i < E.rows && C.n > 0)
-          put<float, 8>(E.part, (int64_t(blockIdx.y) * E.rows + i) * E.cols + C.j, v, C.n);
+          put<float, 4>(E.part, (int64_t(blockIdx.y) * E.rows + i) * E.cols + C.j, v, C.n);
       }
       wave_sync();
     }
@@ -507,27 +517,30 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
   }
   with_type(E.dtype, [&](auto type) {
     typedef decltype(type) O;
-    Vec<O, 8> res[U];
+    constexpr int N = 16 / int(sizeof(O));
+    const Out<N, NJ> L(lds);
+    const Columns<N> C(E, j0 + L.c);
+    Vec<O, N> res[L.U];
     const auto ahead = [&](int a) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = i0 + 16 * a + u * kDown + r;
-        if (!kPlain && i < E.rows && C.n > 0) load_residual<O>(E, C, i, res[u]);
+      for (int u = 0; u < L.U; ++u) {
+        const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
+        if (!kPlain && i < E.rows && C.n > 0) load_residual(E, C, i, res[u]);
       }
     };
     ahead(0);
 #pragma unroll
     for (int a = 0; a < NI; ++a) {
-      exchange(a);
-      Vec<O, 8> now[U];
+      L.exchange(acc[a]);
+      Vec<O, N> now[L.U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) now[u] = res[u];
+      for (int u = 0; u < L.U; ++u) now[u] = res[u];
       if (a + 1 < NI) ahead(a + 1);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = i0 + 16 * a + u * kDown + r;
-        float v[8];
-        take(u, v);
+      for (int u = 0; u < L.U; ++u) {
+        const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
+        float v[N];
+        L.take(u, v);
         if (i < E.rows && C.n > 0) finish<O, kPlain>(E, C, i, now[u], v);
       }
       wave_sync();
@@ -765,40 +778,42 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
 }
 
-// Adds the parts of a product in a fixed order, then the epilogue.  kShare threads share 8
-// neighbours of a row: each adds every kShare-th part, the first adds theirs.
-template <int kShare>
+// Adds the parts of a product in a fixed order, then the epilogue.  kShare threads share N
+// neighbours of a row (16 bytes of it): each adds every kShare-th part, the first adds theirs.
+template <int kShare, int N>
 __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
   constexpr int kAt = 256 / kShare;
-  __shared__ float red[kShare > 1 ? kShare : 1][kShare > 1 ? kAt : 1][9];
-  const int64_t per_row = (E.cols + 7) / 8;
+  __shared__ float red[kShare > 1 ? kShare : 1][kShare > 1 ? kAt : 1][N + 1];
+  const int64_t per_row = (E.cols + N - 1) / N;
   const int share = threadIdx.x / kAt, at = threadIdx.x % kAt;
   const int64_t t = int64_t(blockIdx.x) * kAt + at;
   const bool in = t < E.rows * per_row;
-  const int64_t i = in ? t / per_row : 0, j = in ? t % per_row * 8 : 0;
+  const int64_t i = in ? t / per_row : 0, j = in ? t % per_row * N : 0;
   float *const part = E.part;
   E.part = nullptr;
-  const Columns C(E, j);
-  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const Columns<N> C(E, j);
+  float v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = 0.0f;
 #pragma unroll 4
   for (int s = share; s < splits; s += kShare) {
-    float a[8];
-    get<float, 8>(part, (s * E.rows + i) * E.cols + j, a, C.n);
+    float a[N];
+    get<float, N>(part, (s * E.rows + i) * E.cols + j, a, C.n);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += a[k];
+    for (int k = 0; k < N; ++k) v[k] += a[k];
   }
   if constexpr (kShare > 1) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) red[share][at][k] = v[k];
+    for (int k = 0; k < N; ++k) red[share][at][k] = v[k];
     __syncthreads();
     if (share) return;
     for (int s = 1; s < kShare; ++s)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += red[s][at][k];
+      for (int k = 0; k < N; ++k) v[k] += red[s][at][k];
   }
   if (!in) return;
   with_type(E.dtype, [&](auto type) {
-    Vec<decltype(type), 8> r;
+    Vec<decltype(type), N> r;
     load_residual(E, C, i, r);
     finish<decltype(type), false>(E, C, i, r, v);
   });
@@ -881,7 +896,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
   // 8 neighbours of a row each
   for (int t = threadIdx.x; t < G * 32; t += 64 * kWaves) {
     const int64_t i = t >> 1;
-    const Columns C(A.E, j0 + (t & 1) * 8);
+    const Columns<8> C(A.E, j0 + (t & 1) * 8);
     if (i >= A.E.rows || C.n <= 0) continue;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int s = 0; s < kWaves; ++s)
@@ -1019,7 +1034,7 @@ double filled(int64_t tiles, int64_t at_once) {
   return double(tiles) / double(ceil_div<int64_t>(tiles, at_once) * at_once);
 }
 
-Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both) {
+Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both, bool direct) {
   Plan p{Cut::kMedium, 128, 128, 1, 0, rows};
   if (rows > 0 && cols > 0) {
     const int64_t large = tiles_of(rows, cols, 256, 256), tall = tiles_of(rows, cols, 256, 128);
@@ -1030,7 +1045,12 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both)
       p = Plan{Cut::kLarge, 256, 256, 1, 0, rows};
     else if (medium <= kUnits / 2 && medium * (depth / (32 * slab)) <= kUnits / 2)
       p = Plan{Cut::kSmall, 64, 64, 1, 0, rows};
-    const int64_t at_once = p.cut == Cut::kLarge ? kUnits : 2 * kUnits;
+    // blocks of the small tiles whose slabs go through registers have one slab in LDS, and
+    // one in flight: four on a unit (dx of 6 x 2752 by 2752 x 6874 in float32: 38 us, by
+    // two 51)
+    const int64_t at_once = p.cut == Cut::kLarge                 ? kUnits
+                            : p.cut == Cut::kSmall && !direct ? 4 * kUnits
+                                                              : 2 * kUnits;
     const int64_t tiles = tiles_of(rows, cols, p.tile_i, p.tile_j);
     if (tiles < at_once) {
       // the depth in parts of at least 8 slabs; where half the blocks are there anyway, only
@@ -1063,15 +1083,16 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both)
   p.splits = depth > 0 ? ceil_div<int64_t>(depth, p.per_split) : 1;
   return p;
 }
-// Bytes of the parts of a product, its rows taken plan by plan.
+// Bytes of the parts of a product, its rows taken plan by plan, whatever its operands'
+// alignment.
 int64_t parts_bytes(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both) {
   int64_t most = 0;
-  while (rows > 0 && cols > 0) {
-    const Plan p = plan_of(rows, cols, depth, slab, both);
-    const int64_t bytes = p.splits > 1 ? p.splits * p.rows * cols * 4 : 0;
-    most = bytes > most ? bytes : most;
-    rows -= p.rows;
-  }
+  for (const bool direct : {false, true})
+    for (int64_t left = rows; left > 0 && cols > 0;) {
+      const Plan p = plan_of(left, cols, depth, slab, both, direct);
+      if (p.splits > 1) most = std::max(most, p.splits * p.rows * cols * 4);
+      left -= p.rows;
+    }
   return most;
 }
 
@@ -1153,14 +1174,21 @@ void launch_few(const Product &A, const FewPlan &p, hipStream_t stream) {
     hipLaunchKernelGGL((k_few<S, G, 16>), grid, dim3(1024), 0, stream, A);
 }
 
-hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
-  const int64_t vectors = E.rows * ceil_div<int64_t>(E.cols, 8);
+template <int N>
+void launch_join(const Epilogue &E, int64_t splits, hipStream_t stream) {
+  const int64_t vectors = E.rows * ceil_div<int64_t>(E.cols, N);
   if (splits > 4)
-    hipLaunchKernelGGL(k_join<8>, dim3(unsigned(ceil_div<int64_t>(vectors, 32))), dim3(256), 0,
-                       stream, E, int32_t(splits));
+    hipLaunchKernelGGL((k_join<8, N>), dim3(unsigned(ceil_div<int64_t>(vectors, 32))), dim3(256),
+                       0, stream, E, int32_t(splits));
   else
-    hipLaunchKernelGGL(k_join<1>, dim3(unsigned(ceil_div<int64_t>(vectors, 256))), dim3(256), 0,
-                       stream, E, int32_t(splits));
+    hipLaunchKernelGGL((k_join<1, N>), dim3(unsigned(ceil_div<int64_t>(vectors, 256))), dim3(256),
+                       0, stream, E, int32_t(splits));
+}
+hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
+  if (E.dtype == HG_DT_F32)
+    launch_join<4>(E, splits, stream);
+  else
+    launch_join<8>(E, splits, stream);
   return hipGetLastError();
 }
 
@@ -1206,7 +1234,7 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
   const int64_t slab = kDepth<typename ComputeOf<S>::T, 128>;
   const bool direct = is_direct<S>(P, TP, depth) && is_direct<S>(Q, TQ, depth);
   for (int64_t done = 0; done < E.rows;) {
-    Plan p = plan_of(E.rows - done, E.cols, depth, slab, TP && TQ);
+    Plan p = plan_of(E.rows - done, E.cols, depth, slab, TP && TQ, direct);
     // (any operands: tiles of 128 x 128 or 64 x 64; the parts and rows stay as planned)
     if (!direct && p.cut != Cut::kSmall) p.cut = Cut::kMedium, p.tile_i = p.tile_j = 128;
     Product B = A;
