@@ -394,33 +394,49 @@ struct Columns {
   }
 };
 
-// The columns' sums v of row i, to the result (n > 0; O: its type); `residual`: the row's.
-template <typename O, bool kPlain, int N>
-__device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, int64_t i,
-                                       const Vec<O, N> &residual, float *v) {
+// The columns' sums v of R rows, i and every step-th after it, to the result (n > 0; O: its
+// type); `residual`: the rows'.
+template <typename O, bool kPlain, int N, int R>
+__device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, int64_t i, int step,
+                                       const Vec<O, N> *residual, float (&v)[R][N]) {
+  const auto write = [&](void *to, int64_t stride) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (i + r * step < E.rows)
+        put<O, N, Move::kStreamed>(to, (i + r * step) * stride + C.j, v[r], C.n);
+  };
   if (kPlain) {
-    put<O, N, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
+    write(E.y, E.y_stride);
     return;
   }
   if (E.col_scale) {
-    const float r = E.row_scale[i];
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] *= r * C.scale[k];
+    for (int r = 0; r < R; ++r) {
+      const float by = E.row_scale[min<int64_t>(i + r * step, E.rows - 1)];
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[r][k] *= by * C.scale[k];
+    }
   }
   if (E.bias) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += C.bias[k];
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[r][k] += C.bias[k];
   }
-  if (E.pre) put<O, N, Move::kStreamed>(E.pre, i * E.pre_stride + C.j, v, C.n);
+  if (E.pre) write(E.pre, E.pre_stride);
   with_act(E.act, [&](auto act) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = act_of<decltype(act)::value>(v[k]);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[r][k] = act_of<decltype(act)::value>(v[r][k]);
   });
   if (E.residual) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += float(residual.e[k]);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[r][k] += float(residual[r].e[k]);
   }
-  put<O, N, Move::kStreamed>(E.y, i * E.y_stride + C.j, v, C.n);
+  write(E.y, E.y_stride);
 }
 template <typename O, int N>
 __device__ __forceinline__ void load_residual(const Epilogue &E, const Columns<N> &C, int64_t i,
@@ -519,6 +535,9 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
     typedef decltype(type) O;
     constexpr int N = 16 / int(sizeof(O));
     const Out<N, NJ> L(lds);
+    // two rows for one pass through the epilogue's branches (150001 x 128 x 256 in bfloat16:
+    // 36 us, one row each 39)
+    constexpr int R = L.U < 2 ? L.U : 2;
     const Columns<N> C(E, j0 + L.c);
     Vec<O, N> res[L.U];
     const auto ahead = [&](int a) {
@@ -537,11 +556,12 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
       for (int u = 0; u < L.U; ++u) now[u] = res[u];
       if (a + 1 < NI) ahead(a + 1);
 #pragma unroll
-      for (int u = 0; u < L.U; ++u) {
+      for (int u = 0; u < L.U; u += R) {
         const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
-        float v[N];
-        L.take(u, v);
-        if (i < E.rows && C.n > 0) finish<O, kPlain>(E, C, i, now[u], v);
+        float v[R][N];
+#pragma unroll
+        for (int t = 0; t < R; ++t) L.take(u + t, v[t]);
+        if (i < E.rows && C.n > 0) finish<O, kPlain>(E, C, i, L.kDown, now + u, v);
       }
       wave_sync();
     }
@@ -792,7 +812,8 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
   float *const part = E.part;
   E.part = nullptr;
   const Columns<N> C(E, j);
-  float v[N];
+  float sums[1][N];
+  float *const v = sums[0];
 #pragma unroll
   for (int k = 0; k < N; ++k) v[k] = 0.0f;
 #pragma unroll 4
@@ -815,7 +836,7 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
   with_type(E.dtype, [&](auto type) {
     Vec<decltype(type), N> r;
     load_residual(E, C, i, r);
-    finish<decltype(type), false>(E, C, i, r, v);
+    finish<decltype(type), false>(E, C, i, 0, &r, sums);
   });
 }
 
@@ -898,7 +919,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
     const int64_t i = t >> 1;
     const Columns<8> C(A.E, j0 + (t & 1) * 8);
     if (i >= A.E.rows || C.n <= 0) continue;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float sums[1][8] = {};
+    float *const v = sums[0];
     for (int s = 0; s < kWaves; ++s)
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
@@ -909,7 +931,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
     with_type(A.E.dtype, [&](auto type) {
       Vec<decltype(type), 8> r;
       load_residual(A.E, C, i, r);
-      finish<decltype(type), false>(A.E, C, i, r, v);
+      finish<decltype(type), false>(A.E, C, i, 0, &r, sums);
     });
   }
 }
