@@ -427,9 +427,10 @@ __global__ __launch_bounds__(kBlockOf<G>) void k_distill(hg_distill_args A) {
     }
     const Cut<T, kAlign> C(z, n);
     const T *const body = z + C.head;
-    const int end = C.whole * V;
+    // (counted without a sign: near the end of the longest rows a step passes 2^31)
+    const uint32_t end = C.whole * V;
     Softmax q;
-    int k0 = 0;
+    uint32_t k0 = 0;
     for (; k0 + G * V * U <= end; k0 += G * V * U) {
       Vec<T> r[U];
       float x[U * V];
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(kBlockOf<G>) void k_distill(hg_distill_args A) {
       for (int j = 0; j < V; ++j) x[j] = float(r.e[j]);
       q.add(x, R.c);
     };
-    for (int k = k0 + tid * V; k < end; k += G * V) add(body + k, V);
+    for (uint32_t k = k0 + tid * V; k < end; k += G * V) add(body + k, V);
     if (kAlign && tid == 0 && C.head) add(z, C.head);
     if (tid == 1 && C.last) add(z + n - C.last, C.last);
     R.begin(i);
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(kBlockOf<G>) void k_distill(hg_distill_args A) {
       T *const grad = static_cast<T *>(A.grad) + i * A.grad_stride;
       const bool zero = R.nothing || R.a == 0.0f;
       const float f = R.a * R.inv_t / q.s;
-      const auto slope = [&](int k, int m) {
+      const auto slope = [&](uint32_t k, int m) {
         Vec<T> r;
         r.load(z + k, m);
 #pragma unroll
@@ -464,7 +465,7 @@ __global__ __launch_bounds__(kBlockOf<G>) void k_distill(hg_distill_args A) {
           r.e[j] = T(zero ? 0.0f : f * exp_of(float(r.e[j]), q.m, R.c));
         r.template store<Move::kStreamed>(grad + k, m);
       };
-      for (int k = tid * V; k < end; k += G * V) slope(C.head + k, V);
+      for (uint32_t k = tid * V; k < end; k += G * V) slope(C.head + k, V);
       if (tid == 0 && C.head) slope(0, C.head);
       if (tid == 1 && C.last) slope(n - C.last, C.last);
       R.listed_entries(grad, q);

@@ -255,10 +255,11 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
   constexpr int V = kVec<T>;
   __shared__ float red[Group<kBlock>::kLds];
   Group<kBlock> grp(red);
-  const int dim = int(A.dim);
+  // (counted without a sign: near the end of the longest rows a step passes 2^31)
+  const uint32_t dim = uint32_t(A.dim);
   for (int64_t i = blockIdx.x; i < A.rows; i += gridDim.x) {
     const int64_t at = Source{A.ids, A.x_rows}.at(i);
-    auto load_h = [&](int c, float *h) {
+    auto load_h = [&](uint32_t c, float *h) {
       Vec<T> t;
       load_x<T, Move::kCached>(A.x, A.x_stride, at, c, dim - c, t);
 #pragma unroll
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
       }
     };
     float ss = 0.0f;
-    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
       float h[V];
       load_h(c, h);
 #pragma unroll
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
     float f = 1.0f;
     if (E4M3) {
       uint32_t amax = 0;
-      for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
         float h[V], w[V];
         load_h(c, h);
         load_weight<T>(A, c, dim - c, w);
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
       if (threadIdx.x == 0) A.scale[i] = sc;
     }
     // (a lane reads what it overwrites before it does, and no other lane's)
-    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
       const int n = dim - c;
       float h[V], w[V];
       load_h(c, h);
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
   constexpr int V = kVec<T>;
   __shared__ float red[Group<kBlock>::kLds];
   Group<kBlock> grp(red);
-  const int dim = int(A.dim);
+  const uint32_t dim = uint32_t(A.dim);
   const Source src{A.ids, A.x_rows};
   hg_norm_args N{};
   N.weight = A.weight;
@@ -443,13 +444,13 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
   float *const part =
       A.dweight ? static_cast<float *>(A.workspace) + int64_t(blockIdx.x) * dim : nullptr;
   if (part)
-    for (int c = threadIdx.x * V; c < dim; c += kBlock * V)
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V)
       for (int j = 0; j < V && c + j < dim; ++j) part[c + j] = 0.0f;
   for (int64_t i = blockIdx.x; i < A.rows; i += gridDim.x) {
     const int64_t at = src.at(i);
     const T *const dy = static_cast<const T *>(A.dy) + i * A.dy_stride;
     float ss = 0.0f, gh = 0.0f;
-    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
       float w[V];
       Vec<T> d, x;
       d.load(dy + c, dim - c);
@@ -466,7 +467,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
     const float inv = 1.0f / float(dim);
     const float s = rsqrtf(ss * inv + A.eps);
     const float k = gh * inv * s * s;
-    for (int c = threadIdx.x * V; c < dim; c += kBlock * V) {
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
       const int n = dim - c;
       float w[V], o[V];
       Vec<T> d, x;
