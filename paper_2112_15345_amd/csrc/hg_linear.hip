@@ -684,11 +684,14 @@ struct Stream {
   }
 };
 
-// Waits until at most n of this wavefront's loads are in flight.
+// Waits until at most n of this wavefront's loads are in flight, and none of its reads of LDS: a
+// slab is overwritten behind the barrier that follows, and the products that use the last
+// fragments need not stand before it.  (As compiled they do, and the wait costs nothing.)
 template <int n>
 __device__ __forceinline__ void wait_loads() {
   static_assert(n < 64, "the counter's range");
-  __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | (n >> 4) << 14);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (n & 15) | (n >> 4) << 14);
 }
 
 // Aligned operands: a ring of kStages slabs in LDS, the loads of the next ones in
