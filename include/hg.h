@@ -665,7 +665,9 @@ int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim);
  * and y, pre and residual in out_dtype (float32, float16 or bfloat16).
  * float32 products are made of 16-bit pieces that add up to the elements (of
  * elements below 2^-108 in size the pieces may lose the lower bits), and are
- * as exact as products in 32 bits; 8-bit elements are multiplied as bfloat16.
+ * as exact as products in 32 bits; results that are not finite that way, as
+ * where terms pass the largest float32, are made by products in 32 bits.
+ * 8-bit elements are multiplied as bfloat16.
  * act: gelu is z / (1 + exp(-2 u)), u = sqrt(2/pi) (z + 0.044715 z^3) (its tanh
  * form); silu is z / (1 + exp(-z)).
  * y may be residual with the same stride. */

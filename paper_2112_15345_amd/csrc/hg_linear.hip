@@ -77,7 +77,7 @@ __device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, float) {
 struct Plain32 {};
 
 // Fragments as the matrix instructions take them, kPer of them at a time.
-template <typename S, bool kExact>
+template <typename S>
 struct Step {
   static constexpr int kPer = 1;
   u32x4 v;
@@ -87,8 +87,8 @@ struct Step {
     return hg::mma(c, v, q.v, S());
   }
 };
-template <bool kExact>
-struct Step<F8, kExact> {  // 16 elements: two steps of bfloat16
+template <>
+struct Step<F8> {  // 16 elements: two steps of bfloat16
   static constexpr int kPer = 1;
   u32x4 v[2];
   __device__ __forceinline__ Step() {}
@@ -105,31 +105,24 @@ struct Step<F8, kExact> {  // 16 elements: two steps of bfloat16
 // instructions are 16 times as fast as the 32-bit ones (16385 x 1024 x 4096: 771 us, by the
 // 32-bit instructions 1303).  The pieces are made by integer operations: the conversion
 // instruction is slower than the products it feeds (881 us with it).
-// Infinities and values that round past the largest bfloat16 give NaN pieces, and so a
-// NaN in the result: the caller then starts again with kExact, where those values are one
-// piece (h; nothing in the products of the smaller pieces, where an infinity would meet
-// zeros).  Finite values have the same pieces either way, so that what a NaN does not
-// reach keeps its bits.
-template <bool kExact>
-struct Step<float, kExact> {
+// A result that is finite is one whose terms all were.  Infinities, NaN, values that round past
+// the largest bfloat16 and products of pieces that pass the largest float32 (of either sign, also
+// where the whole product stays below it) end in an infinity or a NaN: the caller makes those
+// results again by the 32-bit instructions, and keeps the others.
+template <>
+struct Step<float> {
   static constexpr int kPer = 2;
-  u32x4 h, m, l, g;  // g: h of the finite values
+  u32x4 h, m, l;
   __device__ __forceinline__ Step() {}
   __device__ __forceinline__ explicit Step(const u32x4 *f) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {  // two elements to a register of each piece
       const uint32_t x = f[e / 2][e % 2 * 2], y = f[e / 2][e % 2 * 2 + 1];
-      uint32_t hx = (x + 0x8000u) & 0xffff0000u, hy = (y + 0x8000u) & 0xffff0000u;
-      float rx = __uint_as_float(x) - __uint_as_float(hx);
-      float ry = __uint_as_float(y) - __uint_as_float(hy);
-      uint32_t gx = hx, gy = hy;
-      if (kExact) {
-        careful(x, hx, rx, gx);
-        careful(y, hy, ry, gy);
-      }
-      h[e] = upper(hx, hy);
-      g[e] = kExact ? upper(gx, gy) : h[e];
+      const uint32_t hx = (x + 0x8000u) & 0xffff0000u, hy = (y + 0x8000u) & 0xffff0000u;
+      const float rx = __uint_as_float(x) - __uint_as_float(hx);
+      const float ry = __uint_as_float(y) - __uint_as_float(hy);
       const uint32_t mx = __float_as_uint(rx) & 0xffff0000u, my = __float_as_uint(ry) & 0xffff0000u;
+      h[e] = upper(hx, hy);
       m[e] = upper(__float_as_uint(rx), __float_as_uint(ry));
       l[e] = upper(__float_as_uint(rx - __uint_as_float(mx)),
                    __float_as_uint(ry - __uint_as_float(my)));
@@ -139,44 +132,11 @@ struct Step<float, kExact> {
   __device__ __forceinline__ static uint32_t upper(uint32_t x, uint32_t y) {
     return __builtin_amdgcn_perm(y, x, 0x07060302u);
   }
-  // h, x - h and g of a value that may not be finite or may round to an infinity.
-  __device__ __forceinline__ static void careful(uint32_t x, uint32_t &h, float &r, uint32_t &g) {
-    const uint32_t size = x & 0x7fffffffu;
-    if (size >= 0x7f800000u) {  // (a NaN's own bits: rounding may carry them away)
-      h = size > 0x7f800000u ? 0x7fc00000u : x;
-      r = 0.0f;
-      g = 0;
-    } else {
-      if ((h & 0x7fffffffu) >= 0x7f800000u) h = x & 0xffff0000u;
-      r = __uint_as_float(x) - __uint_as_float(h);
-      g = h;
-    }
-  }
 };
-
-// One row of 16 x 16 parts.  (32 bits: product by product over the row, since an
-// instruction that adds to what the last one has not finished waits for it.)
-template <typename St, int NJ>
-__device__ __forceinline__ void mma_row(const St (&p)[NJ], const St &q, f32x4 (&c)[NJ]) {
-  if constexpr (St::kPer == 2) {
-    const auto all = [&](u32x4 St::*a, u32x4 b) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) c[j] = mma(c[j], p[j].*a, b, __bf16());
-    };
-    all(&St::l, q.g);
-    all(&St::g, q.l);
-    all(&St::m, q.m);
-    all(&St::m, q.g);
-    all(&St::g, q.m);
-    all(&St::h, q.h);
-  } else {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) c[j] = p[j].mma(q, c[j]);
-  }
-}
-// 64 x 64 tiles of 32-bit elements, where latency counts, use the 32-bit instructions.
+// 32-bit elements by the 32-bit instructions: 64 x 64 tiles, where latency counts, and results that
+// the pieces do not give.
 template <>
-struct Step<Plain32, true> {
+struct Step<Plain32> {
   static constexpr int kPer = 1;
   u32x4 v;
   __device__ __forceinline__ Step() {}
@@ -185,6 +145,27 @@ struct Step<Plain32, true> {
     return hg::mma(c, v, q.v, float());
   }
 };
+
+// One row of 16 x 16 parts.  (Pieces: product by product over the row, since an
+// instruction that adds to what the last one has not finished waits for it.)
+template <typename St, int NJ>
+__device__ __forceinline__ void mma_row(const St (&p)[NJ], const St &q, f32x4 (&c)[NJ]) {
+  if constexpr (St::kPer == 2) {
+    const auto all = [&](u32x4 St::*a, u32x4 b) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) c[j] = mma(c[j], p[j].*a, b, __bf16());
+    };
+    all(&St::l, q.h);
+    all(&St::h, q.l);
+    all(&St::m, q.m);
+    all(&St::m, q.h);
+    all(&St::h, q.m);
+    all(&St::h, q.h);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) c[j] = p[j].mma(q, c[j]);
+  }
+}
 
 // ---- operands ------------------------------------------------------------------
 
@@ -729,8 +710,8 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   const bool idle = i0 + wi >= A.E.rows || j0 + wj >= A.E.cols;  // no part of C for this wavefront
 
   f32x4 acc[NI][NJ];
-  const auto multiply_all = [&](auto exact) {
-    typedef Step<std::conditional_t<kPlain32, Plain32, S>, decltype(exact)::value> St;
+  const auto multiply_all = [&](f32x4 (&acc)[NI][NJ], auto step) {
+    typedef decltype(step) St;
 #pragma unroll
     for (int a = 0; a < NI; ++a)
 #pragma unroll
@@ -783,19 +764,28 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
       }
     }
   };
+  multiply_all(acc, Step<std::conditional_t<kPlain32, Plain32, S>>());
   if constexpr (sizeof(S) == 4 && !kPlain32) {
-    multiply_all(std::false_type());
-    bool nan = false;
+    const auto finite = [](float v) { return fabsf(v) < INFINITY; };
+    bool all = true;
 #pragma unroll
     for (int a = 0; a < NI; ++a)
 #pragma unroll
       for (int b = 0; b < NJ; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) nan = nan || acc[a][b][e] != acc[a][b][e];
+        for (int e = 0; e < 4; ++e) all = all && finite(acc[a][b][e]);
     // (the barrier also says that the ring has been read)
-    if (__syncthreads_or(nan)) multiply_all(std::true_type());
-  } else {
-    multiply_all(std::true_type());
+    if (__syncthreads_or(!all)) {
+      f32x4 again[NI][NJ];
+      multiply_all(again, Step<Plain32>());
+#pragma unroll
+      for (int a = 0; a < NI; ++a)
+#pragma unroll
+        for (int b = 0; b < NJ; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[a][b][e] = finite(acc[a][b][e]) ? acc[a][b][e] : again[a][b][e];
+    }
   }
   __syncthreads();
   write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
@@ -907,9 +897,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
 #pragma unroll
           for (int i = 0; i < G; ++i) acc[i] = mma(acc[i], fw[u][h], fx[u][i][h], S());
         } else {
-          const Step<S, true> p(&fw[u][h]);
+          const Step<S> p(&fw[u][h]);
 #pragma unroll
-          for (int i = 0; i < G; ++i) acc[i] = p.mma(Step<S, true>(&fx[u][i][h]), acc[i]);
+          for (int i = 0; i < G; ++i) acc[i] = p.mma(Step<S>(&fx[u][i][h]), acc[i]);
         }
       }
   }
