@@ -358,6 +358,23 @@ __device__ __forceinline__ void get_as(const void *base, int32_t dtype, int64_t 
     get<__bf16, N>(base, at, v, n);
 }
 
+// Scales of rows and columns: none, mild ones (the product of any two is an ordinary number), or any.
+enum class Scales { kNone, kMild, kAny };
+__device__ __forceinline__ bool is_mild(float s) {
+  return s >= 0x1p-62f && s < 0x1p62f;
+}
+// The product of two scales, which alone may leave float32's range: by mantissas in [1/2, 1) and
+// exponents.  (Infinities and NaN are mantissas.)
+struct Factor {
+  float m;
+  int e;
+  __device__ __forceinline__ Factor() {}
+  __device__ __forceinline__ Factor(float a, float b)
+      : m(__builtin_amdgcn_frexp_mantf(a) * __builtin_amdgcn_frexp_mantf(b)),
+        e(__builtin_amdgcn_frexp_expf(a) + __builtin_amdgcn_frexp_expf(b)) {}
+  __device__ __forceinline__ float times(float v) const { return ldexpf(v * m, e); }
+};
+
 // N columns of C, from j on, n of them in C: what is the same for every row.
 template <int N>
 struct Columns {
@@ -375,9 +392,26 @@ struct Columns {
   }
 };
 
+// The scales on the columns' sums v of R rows, i and every step-th after it.
+// (By mantissas and exponents for all, the 8-bit batch took 422 us, with the mild ones apart 416.)
+template <Scales kScales, int N, int R>
+__device__ __forceinline__ void scale(const Epilogue &E, const Columns<N> &C, int64_t i, int step,
+                                      float (&v)[R][N]) {
+  if constexpr (kScales != Scales::kNone) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float by = E.row_scale[min<int64_t>(i + r * step, E.rows - 1)];
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        v[r][k] = kScales == Scales::kMild ? v[r][k] * (by * C.scale[k])
+                                           : Factor(by, C.scale[k]).times(v[r][k]);
+    }
+  }
+}
+
 // The columns' sums v of R rows, i and every step-th after it, to the result (n > 0; O: its
 // type); `residual`: the rows'.
-template <typename O, bool kPlain, int N, int R>
+template <typename O, bool kPlain, Scales kScales, int N, int R>
 __device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, int64_t i, int step,
                                        const Vec<O, N> *residual, float (&v)[R][N]) {
   const auto write = [&](void *to, int64_t stride) {
@@ -390,14 +424,7 @@ __device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, i
     write(E.y, E.y_stride);
     return;
   }
-  if (E.col_scale) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float by = E.row_scale[min<int64_t>(i + r * step, E.rows - 1)];
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[r][k] *= by * C.scale[k];
-    }
-  }
+  scale<kScales>(E, C, i, step, v);
   if (E.bias) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -465,7 +492,7 @@ __device__ __forceinline__ void tile_of(const Product &A, int64_t b, int64_t &ti
 // 8 neighbours in 32 bits, two stores to a lane's 32 bytes, the halves of lines went out by
 // themselves (the gradient of 4096 x 4096 weights over 8 rows: 36 us, now 20).  A lane keeps its columns; the residual
 // is loaded 16 rows ahead.
-// kPlain: nothing but the sums (the gradients).
+// kPlain: nothing but the sums (the gradients).  kScaled: with scales, mild ones or not.
 template <int N, int NJ>
 struct Out {
   static constexpr int WJ = NJ * 16;
@@ -490,9 +517,9 @@ struct Out {
           *reinterpret_cast<const f32x4 *>(out + (u * kDown + r) * LD + c + h);
   }
 };
-template <bool kPlain, int NI, int NJ>
+template <bool kPlain, bool kScaled, int NI, int NJ>
 __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i0, int64_t j0,
-                                          const f32x4 (&acc)[NI][NJ]) {
+                                          const f32x4 (&acc)[NI][NJ], bool mild) {
   const Epilogue &E = A.E;
   if (E.part) {
     const Out<4, NJ> L(lds);
@@ -512,7 +539,7 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
     }
     return;
   }
-  with_type(E.dtype, [&](auto type) {
+  const auto write = [&](auto type, auto scales) {
     typedef decltype(type) O;
     constexpr int N = 16 / int(sizeof(O));
     const Out<N, NJ> L(lds);
@@ -534,7 +561,15 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
       L.exchange(acc[a]);
       Vec<O, N> now[L.U];
 #pragma unroll
-      for (int u = 0; u < L.U; ++u) now[u] = res[u];
+      for (int u = 0; u < L.U; ++u) {
+        now[u] = res[u];
+        if (!kPlain) {  // (waited for here, not behind these rows' stores: 133 us, 138 without
+                        // in 65537 x 512 x 1024 with residual and pre)
+          u32x4 raw = __builtin_bit_cast(u32x4, now[u]);
+          asm volatile("" : "+v"(raw));
+          now[u] = __builtin_bit_cast(Vec<O, N>, raw);
+        }
+      }
       if (a + 1 < NI) ahead(a + 1);
 #pragma unroll
       for (int u = 0; u < L.U; u += R) {
@@ -542,11 +577,34 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
         float v[R][N];
 #pragma unroll
         for (int t = 0; t < R; ++t) L.take(u + t, v[t]);
-        if (i < E.rows && C.n > 0) finish<O, kPlain>(E, C, i, L.kDown, now + u, v);
+        if (i < E.rows && C.n > 0)
+          finish<O, kPlain, decltype(scales)::value>(E, C, i, L.kDown, now + u, v);
       }
       wave_sync();
     }
+  };
+  with_type(E.dtype, [&](auto type) {
+    if constexpr (!kScaled)
+      write(type, std::integral_constant<Scales, Scales::kNone>());
+    else if (mild)
+      write(type, std::integral_constant<Scales, Scales::kMild>());
+    else
+      write(type, std::integral_constant<Scales, Scales::kAny>());
   });
+}
+
+// Whether all scales of a wavefront's part of C are mild.
+template <int NI, int NJ>
+__device__ __forceinline__ bool all_mild(const Epilogue &E, int64_t i0, int64_t j0) {
+  const int lane = threadIdx.x & 63;
+  bool mild = true;
+#pragma unroll
+  for (int t = 0; t < 16 * NI; t += 64)
+    mild = mild && is_mild(E.row_scale[min<int64_t>(i0 + t + lane, E.rows - 1)]);
+#pragma unroll
+  for (int t = 0; t < 16 * NJ; t += 64)
+    mild = mild && is_mild(E.col_scale[min<int64_t>(j0 + t + lane, E.cols - 1)]);
+  return __all(mild);
 }
 
 // Any operands: slabs through registers.
@@ -555,6 +613,7 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
   typedef typename ComputeOf<S>::T T;
   constexpr int WI = BI / 2, WJ = BJ / 2;  // a wavefront's part: four, 2 x 2
   constexpr int NI = WI / 16, NJ = WJ / 16;
+  constexpr bool kScaled = std::is_same_v<S, F8>;
   using SP = Slab<T, TP, BJ, 128>;
   using SQ = Slab<T, TQ, BI, 128>;
   constexpr int kStage = SP::kBytes + SQ::kBytes;
@@ -613,7 +672,9 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
         for (int b = 0; b < NJ; ++b) acc[a][b] = mma(acc[a][b], fp[b][h], fq[a][h], T());
   }
   __syncthreads();
-  write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
+  bool mild = true;
+  if constexpr (kScaled) mild = all_mild<NI, NJ>(A.E, i0 + wi, j0 + wj);
+  write_out<TP, kScaled>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
 
 // 16 bytes of zeros: where lanes past an operand's end load from.
@@ -687,6 +748,7 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   constexpr int kWaves = kWavesI * kWavesJ;
   constexpr int WI = BI / kWavesI, WJ = BJ / kWavesJ;
   constexpr int NI = WI / 16, NJ = WJ / 16;
+  constexpr bool kScaled = std::is_same_v<S, F8>;
   using SP = Slab<S, TP, BJ, W>;
   using SQ = Slab<S, TQ, BI, W>;
   using LP = Stream<S, TP, BJ, W, kWaves>;
@@ -707,6 +769,8 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   const int slabs = whole + (rest > 0);
   const int wi = wave / kWavesJ * WI, wj = wave % kWavesJ * WJ;
 
+  bool mild = true;  // (found out here, before there is anything to wait for)
+  if constexpr (kScaled) mild = all_mild<NI, NJ>(A.E, i0 + wi, j0 + wj);
   const bool idle = i0 + wi >= A.E.rows || j0 + wj >= A.E.cols;  // no part of C for this wavefront
 
   f32x4 acc[NI][NJ];
@@ -788,12 +852,12 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
     }
   }
   __syncthreads();
-  write_out<TP>(A, lds, i0 + wi, j0 + wj, acc);
+  write_out<TP, kScaled>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
 
 // Adds the parts of a product in a fixed order, then the epilogue.  kShare threads share N
 // neighbours of a row (16 bytes of it): each adds every kShare-th part, the first adds theirs.
-template <int kShare, int N>
+template <int kShare, int N, Scales kScales>
 __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
   constexpr int kAt = 256 / kShare;
   __shared__ float red[kShare > 1 ? kShare : 1][kShare > 1 ? kAt : 1][N + 1];
@@ -826,10 +890,11 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
       for (int k = 0; k < N; ++k) v[k] += red[s][at][k];
   }
   if (!in) return;
+  scale<kScales>(E, C, i, 0, sums);
   with_type(E.dtype, [&](auto type) {
     Vec<decltype(type), N> r;
     load_residual(E, C, i, r);
-    finish<decltype(type), false>(E, C, i, 0, &r, sums);
+    finish<decltype(type), false, Scales::kNone>(E, C, i, 0, &r, sums);
   });
 }
 
@@ -903,30 +968,40 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
         }
       }
   }
+  // 8 neighbours of a row for a thread; what they meet is loaded before the sums are there
+  const int t = threadIdx.x;
+  const int64_t i = t >> 1;
+  const bool in = t < G * 32 && i < A.E.rows;
+  const Columns<8> C(A.E, in ? j0 + (t & 1) * 8 : A.E.cols);
+  Factor scales[8];
+  if constexpr (std::is_same_v<S, F8>) {
+    const float by = in ? A.E.row_scale[i] : 0.0f;
 #pragma unroll
-  for (int i = 0; i < G; ++i)
-    *reinterpret_cast<f32x4 *>(&red[wave][i][x][4 * g]) = acc[i];
-  __syncthreads();
-  // 8 neighbours of a row each
-  for (int t = threadIdx.x; t < G * 32; t += 64 * kWaves) {
-    const int64_t i = t >> 1;
-    const Columns<8> C(A.E, j0 + (t & 1) * 8);
-    if (i >= A.E.rows || C.n <= 0) continue;
-    float sums[1][8] = {};
-    float *const v = sums[0];
-    for (int s = 0; s < kWaves; ++s)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
-    if (A.E.part) {
-      put<float, 8>(A.E.part, (int64_t(blockIdx.y) * A.E.rows + i) * A.E.cols + C.j, v, C.n);
-      continue;
-    }
-    with_type(A.E.dtype, [&](auto type) {
-      Vec<decltype(type), 8> r;
-      load_residual(A.E, C, i, r);
-      finish<decltype(type), false>(A.E, C, i, 0, &r, sums);
-    });
+    for (int k = 0; k < 8; ++k) scales[k] = Factor(by, C.scale[k]);
   }
+#pragma unroll
+  for (int u = 0; u < G; ++u)
+    *reinterpret_cast<f32x4 *>(&red[wave][u][x][4 * g]) = acc[u];
+  __syncthreads();
+  if (C.n <= 0) return;
+  float sums[1][8] = {};
+  float *const v = sums[0];
+  for (int s = 0; s < kWaves; ++s)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
+  if (A.E.part) {
+    put<float, 8>(A.E.part, (int64_t(blockIdx.y) * A.E.rows + i) * A.E.cols + C.j, v, C.n);
+    return;
+  }
+  if constexpr (std::is_same_v<S, F8>) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = scales[k].times(v[k]);
+  }
+  with_type(A.E.dtype, [&](auto type) {
+    Vec<decltype(type), 8> r;
+    load_residual(A.E, C, i, r);
+    finish<decltype(type), false, Scales::kNone>(A.E, C, i, 0, &r, sums);
+  });
 }
 
 // ---- dz and its column sums ------------------------------------------------------
@@ -1189,21 +1264,24 @@ void launch_few(const Product &A, const FewPlan &p, hipStream_t stream) {
     hipLaunchKernelGGL((k_few<S, G, 16>), grid, dim3(1024), 0, stream, A);
 }
 
-template <int N>
+template <int N, Scales kScales>
 void launch_join(const Epilogue &E, int64_t splits, hipStream_t stream) {
   const int64_t vectors = E.rows * ceil_div<int64_t>(E.cols, N);
   if (splits > 4)
-    hipLaunchKernelGGL((k_join<8, N>), dim3(unsigned(ceil_div<int64_t>(vectors, 32))), dim3(256),
-                       0, stream, E, int32_t(splits));
+    hipLaunchKernelGGL((k_join<8, N, kScales>), dim3(unsigned(ceil_div<int64_t>(vectors, 32))),
+                       dim3(256), 0, stream, E, int32_t(splits));
   else
-    hipLaunchKernelGGL((k_join<1, N>), dim3(unsigned(ceil_div<int64_t>(vectors, 256))), dim3(256),
-                       0, stream, E, int32_t(splits));
+    hipLaunchKernelGGL((k_join<1, N, kScales>), dim3(unsigned(ceil_div<int64_t>(vectors, 256))),
+                       dim3(256), 0, stream, E, int32_t(splits));
 }
 hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
-  if (E.dtype == HG_DT_F32)
-    launch_join<4>(E, splits, stream);
+  const bool wide = E.dtype == HG_DT_F32;
+  if (E.col_scale)
+    wide ? launch_join<4, Scales::kAny>(E, splits, stream)
+         : launch_join<8, Scales::kAny>(E, splits, stream);
   else
-    launch_join<8>(E, splits, stream);
+    wide ? launch_join<4, Scales::kNone>(E, splits, stream)
+         : launch_join<8, Scales::kNone>(E, splits, stream);
   return hipGetLastError();
 }
 
