@@ -76,8 +76,8 @@ COUNTER_TRAFFIC = [
 ]
 
 
-DENSE_SOURCES = ("hg_dense.cpp", "hg_dense.hpp", "hg_dense_py.cpp", "hg_distill.hip",
-                 "hg_linear.hip", "hg_norm.hip")
+DENSE_SOURCES = ("hg_dense.cpp", "hg_dense.hpp", "hg_dense_plan.hpp", "hg_dense_py.cpp",
+                 "hg_distill.hip", "hg_linear.hip", "hg_norm.hip")
 
 
 def kernel_sources_digest():

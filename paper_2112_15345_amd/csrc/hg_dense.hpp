@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "hg.h"
+#include "hg_dense_plan.hpp"
 #include "hg_internal.hpp"
 
 namespace hg {
@@ -17,10 +18,8 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-template <typename T>
-__host__ __device__ inline T ceil_div(T a, T b) {
-  return (a + b - 1) / b;
-}
+// Blocks of a launch that walks over its work, at most.  (A grid has fewer than 2^32 threads.)
+constexpr int64_t kMostBlocks = int64_t(1) << 20;
 
 // ---- launchers (all asynchronous on `stream`; arguments already checked) ----
 

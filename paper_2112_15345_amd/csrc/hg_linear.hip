@@ -11,6 +11,7 @@
 // 16 x 16 matrix instructions whose first operand is P, so that a lane ends with 4
 // neighbours of a row of C.
 #include "hg_dense.hpp"
+#include "hg_dense_plan.hpp"
 #include "hg_device.hpp"
 
 namespace hg {
@@ -904,7 +905,6 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
 // (columns of C) and every kWaves-th 128 bytes of them, straight from memory into the
 // matrix instructions' registers, several loads ahead; a block's wavefronts are added in
 // LDS.  G: 16-row parts of x.
-constexpr int64_t kFew = 32;
 
 // 16 bytes of a row of n elements from element c on; zeros past its end.
 template <typename S>
@@ -1006,63 +1006,65 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
 
 // ---- dz and its column sums ------------------------------------------------------
 
-constexpr int kSumRows = 64;  // rows of C that one part of the column sums covers
-
 // dz = dy act'(pre) in T (dz NULL: not written), zeros from column n to its stride, and the
 // sums over the block's rows.
 // A wavefront takes 64 vectors of 8 columns; the block's four take turns over the rows.
-// Block b: columns b % strips, rows b / strips.
+// Place b: columns b % strips, rows b / strips; a block takes every gridDim.x-th place.
 template <typename T>
 __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, const T *pre,
                                             int64_t pre_stride, int32_t act, int64_t m, int64_t n,
-                                            int64_t strips, T *dz, int64_t dz_stride, float *part) {
+                                            int64_t strips, int64_t places, T *dz, int64_t dz_stride,
+                                            float *part) {
   __shared__ float red[4][64 * 8 + 8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t strip = blockIdx.x % strips, chunk = blockIdx.x / strips;
-  const int64_t j = (strip * 64 + lane) * 8;
-  const int64_t r0 = chunk * kSumRows, r1 = min(m, r0 + kSumRows);
-  const int left = int(min<int64_t>(8, n - j)), wide = int(min<int64_t>(8, dz_stride - j));
-  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  constexpr int U = 4;  // rows in flight
-  if (left > 0)
-    for (int64_t i0 = r0 + wave; i0 < r1; i0 += 4 * U) {
-      Vec<T, 8> d[U], z[U];
+  for (int64_t b = blockIdx.x; b < places; b += gridDim.x) {
+    const int64_t strip = b % strips, chunk = b / strips;
+    const int64_t j = (strip * 64 + lane) * 8;
+    const int64_t r0 = chunk * kSumRows, r1 = min(m, r0 + kSumRows);
+    const int left = int(min<int64_t>(8, n - j)), wide = int(min<int64_t>(8, dz_stride - j));
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    constexpr int U = 4;  // rows in flight
+    if (left > 0)
+      for (int64_t i0 = r0 + wave; i0 < r1; i0 += 4 * U) {
+        Vec<T, 8> d[U], z[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = i0 + 4 * u;
-        if (i < r1) {
-          d[u].template load<Move::kStreamed>(dy + i * dy_stride + j, left);
-          if (pre) z[u].template load<Move::kStreamed>(pre + i * pre_stride + j, left);
+        for (int u = 0; u < U; ++u) {
+          const int64_t i = i0 + 4 * u;
+          if (i < r1) {
+            d[u].template load<Move::kStreamed>(dy + i * dy_stride + j, left);
+            if (pre) z[u].template load<Move::kStreamed>(pre + i * pre_stride + j, left);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t i = i0 + 4 * u;
+          if (i >= r1) break;
+          float v[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = float(d[u].e[k]);
+          with_act(act, [&](auto a) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= act_slope<decltype(a)::value>(float(z[u].e[k]));
+          });
+          if (left < 8) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = k < left ? v[k] : 0.0f;
+          }
+          if (dz) put<T, 8>(dz, i * dz_stride + j, v, wide);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[k] += v[k];
         }
       }
+    if (!part) continue;
+    if (b != blockIdx.x) __syncthreads();  // the last place's sums have been read
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t i = i0 + 4 * u;
-        if (i >= r1) break;
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = float(d[u].e[k]);
-        with_act(act, [&](auto a) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] *= act_slope<decltype(a)::value>(float(z[u].e[k]));
-        });
-        if (left < 8) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = k < left ? v[k] : 0.0f;
-        }
-        if (dz) put<T, 8>(dz, i * dz_stride + j, v, wide);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s[k] += v[k];
-      }
+    for (int k = 0; k < 8; ++k) red[wave][lane * 8 + k] = s[k];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 512; c += 256) {
+      const int64_t col = strip * 512 + c;
+      if (col < n)
+        part[chunk * n + col] = red[0][c] + red[1][c] + red[2][c] + red[3][c];
     }
-  if (!part) return;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) red[wave][lane * 8 + k] = s[k];
-  __syncthreads();
-  for (int c = threadIdx.x; c < 512; c += 256) {
-    const int64_t col = strip * 512 + c;
-    if (col < n)
-      part[chunk * n + col] = red[0][c] + red[1][c] + red[2][c] + red[3][c];
   }
 }
 
@@ -1088,104 +1090,6 @@ __global__ __launch_bounds__(256) void k_lay(const S *from, int64_t stride, int6
 
 // ---- launches --------------------------------------------------------------------
 
-int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
-int64_t size_of(int32_t dtype) {
-  return dtype == HG_DT_F32 ? 4 : (dtype == HG_DT_E4M3 ? 1 : 2);
-}
-// Elements of q in 128 bytes of what the matrix instructions take.
-int64_t slab_of(int32_t dtype) { return dtype == HG_DT_F32 ? 32 : 64; }
-
-// How a product is cut: its tiles, how many slabs are in LDS, and the parts of its depth.
-// A compute unit that multiplies one tile waits for its loads unless several slabs are in
-// flight; with two tiles each covers the other's waits.
-//  kLarge   256 x 256, 2 slabs, one block on a unit: 1.28 PF/s in 16 bits at 8192^3.  Not
-//           for depths below 8 slabs (150001 x 128 x 256: 36 us, kMedium 33) nor in 32 bits,
-//           whose products take too long for its uneven last round
-//  kMedium  128 x 128, 2 slabs, two blocks: loading a slab takes as long as multiplying it
-//           (64 bytes a clock), 1.0 PF/s at 8192^3, but its tiles fill the units better
-//  kSmall   64 x 64, 4 slabs, two blocks: for too few tiles of the others (1024^3: 8.8 us,
-//           kMedium 18), unless the depth is long enough to be cut (rows of 512 and 1024
-//           columns' gradient over 65537 rows: 172 us, kMedium 112)
-//  kTall    256 x 128 in slabs of 64 bytes, two blocks: the weight gradients' operands,
-//           whose slabs are read across (8192^3: 1.20 PF/s, kLarge 1.11, kMedium 1.04)
-enum class Cut { kLarge, kMedium, kSmall, kTall };
-struct Plan {
-  Cut cut;
-  int64_t tile_i, tile_j, splits, per_split;
-  int64_t rows;  // of C that this plan is for; the rest have one of their own
-};
-constexpr int64_t kUnits = 256;
-
-int64_t tiles_of(int64_t rows, int64_t cols, int64_t ti, int64_t tj) {
-  return ceil_div<int64_t>(rows, ti) * ceil_div<int64_t>(cols, tj);
-}
-// The share of the last round of blocks that is full, over all rounds.
-double filled(int64_t tiles, int64_t at_once) {
-  return double(tiles) / double(ceil_div<int64_t>(tiles, at_once) * at_once);
-}
-
-Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both, bool direct) {
-  Plan p{Cut::kMedium, 128, 128, 1, 0, rows};
-  if (rows > 0 && cols > 0) {
-    const int64_t large = tiles_of(rows, cols, 256, 256), tall = tiles_of(rows, cols, 256, 128);
-    const int64_t medium = tiles_of(rows, cols, 128, 128);
-    if (both && tall >= kUnits && slab == 64)
-      p = Plan{Cut::kTall, 256, 128, 1, 0, rows};
-    else if (!both && large >= 2 * kUnits && depth >= 8 * slab && slab == 64)
-      p = Plan{Cut::kLarge, 256, 256, 1, 0, rows};
-    else if (medium <= kUnits / 2 && medium * (depth / (32 * slab)) <= kUnits / 2)
-      p = Plan{Cut::kSmall, 64, 64, 1, 0, rows};
-    // blocks of the small tiles whose slabs go through registers have one slab in LDS, and
-    // one in flight: four on a unit (dx of 6 x 2752 by 2752 x 6874 in float32: 38 us, by
-    // two 51)
-    const int64_t at_once = p.cut == Cut::kLarge                 ? kUnits
-                            : p.cut == Cut::kSmall && !direct ? 4 * kUnits
-                                                              : 2 * kUnits;
-    const int64_t tiles = tiles_of(rows, cols, p.tile_i, p.tile_j);
-    if (tiles < at_once) {
-      // the depth in parts of at least 8 slabs; where half the blocks are there anyway, only
-      // a depth that is long next to the writing and adding of the parts: as many that their
-      // rounds take least, a part's writing and adding taken as 1/32 of a slab (5408 x 912
-      // over 26506 rows in float32, 344 tiles: 1825 us as 4 parts each, 2354 as one)
-      const bool most_there = 2 * tiles >= at_once;
-      const int64_t long_ = p.cut == Cut::kSmall ? 16 * slab : 64 * slab;
-      const int64_t most = depth / (most_there ? long_ : 8 * slab);
-      if (most_there) {
-        double least = 0.0;
-        for (int64_t s = 1; s <= std::min<int64_t>(8, most); ++s) {
-          const double t = double(ceil_div<int64_t>(tiles * s, at_once)) * double(depth) /
-                               double(s * slab) + (s > 1 ? 8.0 + double(s * tiles) / 32.0 : 0.0);
-          if (s == 1 || t < least) p.splits = s, least = t;
-        }
-      } else {
-        const int64_t want = std::min<int64_t>(at_once / tiles, 256);
-        p.splits = std::max<int64_t>(1, std::min(want, most));
-      }
-    } else if (tiles <= 6 * at_once && filled(tiles, at_once) < 0.9 && depth >= 16 * slab) {
-      // the rows of whole rounds; the last round's few tiles would leave most units idle
-      // for as long as a full one takes, and are cut finer
-      const int64_t down = tiles / at_once * at_once / ceil_div<int64_t>(cols, p.tile_j);
-      if (down > 0) p.rows = down * p.tile_i;
-    }
-  }
-  p.per_split = ceil_div<int64_t>(ceil_div<int64_t>(depth, slab), p.splits) * slab;
-  if (p.per_split < slab) p.per_split = slab;
-  p.splits = depth > 0 ? ceil_div<int64_t>(depth, p.per_split) : 1;
-  return p;
-}
-// Bytes of the parts of a product, its rows taken plan by plan, whatever its operands'
-// alignment.
-int64_t parts_bytes(int64_t rows, int64_t cols, int64_t depth, int64_t slab, bool both) {
-  int64_t most = 0;
-  for (const bool direct : {false, true})
-    for (int64_t left = rows; left > 0 && cols > 0;) {
-      const Plan p = plan_of(left, cols, depth, slab, both, direct);
-      if (p.splits > 1) most = std::max(most, p.splits * p.rows * cols * 4);
-      left -= p.rows;
-    }
-  return most;
-}
-
 // Whether every 16-byte piece of an operand is aligned, and lies in it or outside it, or
 // ends in zeros.
 template <typename S>
@@ -1195,23 +1099,6 @@ bool is_direct(const Operand &O, bool turned, int64_t depth) {
          (O.padded || (turned ? O.rows : depth) % E == 0);
 }
 
-// The elements of a row laid out in whole pieces.
-int64_t padded(int64_t cols, int64_t size) { return align16(cols * size) / size; }
-
-// Whether a product's operands whose rows are not whole 16-byte pieces are first copied
-// into rows that are, for the kernel of aligned operands: where the product is large and
-// every element is used often enough (us, forward / dx / dw, without and with the copies):
-//   bfloat16  13222 x 2594 x 3968  401 / 630 / 865, 335 / 325 / 359
-//              4096 x  255 x 4097   41 / 128 /  82,  41 /  64 /  68
-//             16385 x  515 x  515   29 /  45 /  95,  45 /  50 /  69
-//              1000 x 1001 x 1003   15 /  21 /  30,  20 /  34 /  35
-//   float32   13222 x 2594 x 3968  2363 / 2669 / 2969, 1708 / 1660 / 1719
-//              1000 x 1001 x 1003   37 /  47 /  51,  42 /  52 /  52
-// (Operands of 16 GiB and more are not copied.)
-bool is_laid(int64_t m, int64_t k, int64_t n, int64_t size) {
-  return std::min(m, std::min(k, n)) >= 250 && double(m) * double(k) * double(n) >= 4e9 &&
-         double(std::max(m, n)) * double(padded(k, size) * size) < 1.6e10;
-}
 // Copies an operand of rows x cols to `to`.
 template <typename S>
 hipError_t lay(Operand &O, int64_t rows, int64_t cols, bool turned, char *to, hipStream_t stream) {
@@ -1230,29 +1117,6 @@ template <typename S, bool TP, bool TQ, int BI, int BJ, int kWavesI, int kWavesJ
 void launch_direct(const Product &A, dim3 grid, hipStream_t stream) {
   hipLaunchKernelGGL((k_product_direct<S, TP, TQ, BI, BJ, kWavesI, kWavesJ, W, kStages>), grid,
                      dim3(64 * kWavesI * kWavesJ), 0, stream, A);
-}
-
-// (A grid has fewer than 2^32 threads.)
-bool is_few(int64_t rows, int64_t cols) { return rows <= kFew && cols <= int64_t(1) << 26; }
-
-// Few rows: blocks of 4 wavefronts, or of 16 where there are few columns; with very few,
-// the depth is cut too, in parts of at least two steps of 128 bytes for a wavefront.
-struct FewPlan {
-  int64_t blocks, waves, splits, per_split;
-};
-FewPlan few_plan(int64_t cols, int64_t depth, int64_t size) {
-  FewPlan p;
-  p.blocks = ceil_div<int64_t>(cols, 16);
-  p.waves = p.blocks >= 512 ? 4 : 16;
-  const int64_t step = p.waves * (128 / size);
-  const int64_t want = p.blocks < 128 && p.blocks > 0 ? 256 / p.blocks : 1;
-  const int64_t most = depth / (2 * step);
-  p.splits = want < most ? want : most;
-  if (p.splits < 1) p.splits = 1;
-  p.per_split = ceil_div<int64_t>(ceil_div<int64_t>(depth, step), p.splits) * step;
-  if (p.per_split < step) p.per_split = step;
-  p.splits = depth > 0 ? ceil_div<int64_t>(depth, p.per_split) : 1;
-  return p;
 }
 
 template <typename S, int G>
@@ -1285,20 +1149,34 @@ hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The operand of the rows of C from row `at` on, and the epilogue of n of them.
+// The operand of C's rows (or columns) from `at` on, and the epilogue of n of them.
 template <typename S>
-Operand rows_from(Operand Q, bool turned, int64_t at) {
-  Q.p = static_cast<const S *>(Q.p) + (turned ? at : at * Q.stride);
-  Q.rows -= at;
-  return Q;
+Operand axis_from(Operand O, bool turned, int64_t at) {
+  O.p = static_cast<const S *>(O.p) + (turned ? at : at * O.stride);
+  O.rows -= at;
+  return O;
 }
-Epilogue epilogue_from(Epilogue E, int64_t at, int64_t n) {
-  const int64_t size = size_of(E.dtype);
+void advance(const void *&p, int64_t elements, int32_t dtype) {
+  if (p) p = static_cast<const char *>(p) + elements * size_of(dtype);
+}
+void advance(void *&p, int64_t elements, int32_t dtype) {
+  if (p) p = static_cast<char *>(p) + elements * size_of(dtype);
+}
+Epilogue epilogue_of_rows(Epilogue E, int64_t at, int64_t n) {
   E.rows = n;
-  E.y = static_cast<char *>(E.y) + at * E.y_stride * size;
-  if (E.residual) E.residual = static_cast<const char *>(E.residual) + at * E.residual_stride * size;
-  if (E.pre) E.pre = static_cast<char *>(E.pre) + at * E.pre_stride * size;
+  advance(E.y, at * E.y_stride, E.dtype);
+  advance(E.residual, at * E.residual_stride, E.dtype);
+  advance(E.pre, at * E.pre_stride, E.dtype);
   if (E.row_scale) E.row_scale += at;
+  return E;
+}
+Epilogue epilogue_of_cols(Epilogue E, int64_t at, int64_t n) {
+  E.cols = n;
+  advance(E.y, at, E.dtype);
+  advance(E.residual, at, E.dtype);
+  advance(E.pre, at, E.dtype);
+  advance(E.bias, at, E.bias_dtype);
+  if (E.col_scale) E.col_scale += at;
   return E;
 }
 
@@ -1324,17 +1202,22 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
       return e != hipSuccess || p.splits == 1 ? e : join(A.E, p.splits, stream);
     }
   }
+  if (E.cols > kMostCols) {
+    const int64_t half = E.cols / 2 / 256 * 256;
+    const hipError_t e = product<S, TP, TQ>(P, Q, depth, epilogue_of_cols(E, 0, half), parts, stream);
+    return e != hipSuccess ? e
+                           : product<S, TP, TQ>(axis_from<S>(P, TP, half), Q, depth,
+                                                epilogue_of_cols(E, half, E.cols - half), parts,
+                                                stream);
+  }
   const int64_t slab = kDepth<typename ComputeOf<S>::T, 128>;
   const bool direct = is_direct<S>(P, TP, depth) && is_direct<S>(Q, TQ, depth);
   for (int64_t done = 0; done < E.rows;) {
-    Plan p = plan_of(E.rows - done, E.cols, depth, slab, TP && TQ, direct);
-    // (any operands: tiles of 128 x 128 or 64 x 64; the parts and rows stay as planned)
-    if (!direct && p.cut != Cut::kSmall) p.cut = Cut::kMedium, p.tile_i = p.tile_j = 128;
+    const Plan p = plan_of(E.rows - done, E.cols, depth, slab, TP && TQ, direct);
     Product B = A;
-    B.Q = rows_from<S>(Q, TQ, done);
-    B.E = epilogue_from(E, done, p.rows);
+    B.Q = axis_from<S>(Q, TQ, done);
+    B.E = epilogue_of_rows(E, done, p.rows);
     const int64_t ti = ceil_div<int64_t>(p.rows, p.tile_i), tj = ceil_div<int64_t>(E.cols, p.tile_j);
-    if (ti * tj * 512 >= int64_t(1) << 32) return hipErrorInvalidConfiguration;  // threads of a grid
     B.tiles_i = int32_t(ti);
     B.tiles_j = int32_t(tj);
     B.per_split = p.per_split;
@@ -1360,27 +1243,6 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
     done += p.rows;
   }
   return hipSuccess;
-}
-
-struct LinearSpace {  // byte offsets in the workspace
-  int64_t w, x, parts, total;
-  bool laid;
-};
-LinearSpace linear_space(int64_t m, int64_t k, int64_t n, int32_t dtype) {
-  LinearSpace s{0, 0, 0, 0, false};
-  if (is_few(m, n)) {
-    const int64_t splits = few_plan(n, k, size_of(dtype)).splits;
-    s.total = splits > 1 ? splits * m * n * 4 : 0;
-    return s;
-  }
-  const int64_t size = size_of(dtype), row = padded(k, size);
-  s.laid = row != k && is_laid(m, k, n, size);
-  if (s.laid) {
-    s.x = n * row * size;
-    s.parts = s.x + m * row * size;
-  }
-  s.total = s.parts + parts_bytes(m, n, k, slab_of(dtype), false);
-  return s;
 }
 
 template <typename T>
@@ -1413,28 +1275,6 @@ hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
   return product<T, false, false>(w, x, A.k, E, reinterpret_cast<float *>(ws + s.parts), stream);
 }
 
-struct GradSpace {  // byte offsets in the workspace
-  int64_t dz, sums, x, w, parts, total;
-  int64_t dz_stride;  // of dz in the workspace
-  bool dz_laid, laid;
-};
-GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
-  GradSpace g;
-  const int64_t slab = slab_of(dtype);
-  const int64_t size = size_of(dtype), row = padded(k, size);
-  g.dz = 0;
-  g.dz_stride = padded(n, size);
-  g.laid = row != k && is_laid(m, k, n, size);
-  g.dz_laid = act != HG_ACT_NONE || (g.dz_stride != n && is_laid(m, k, n, size));
-  g.sums = g.dz_laid ? m * g.dz_stride * size : 0;
-  g.x = g.sums + align16(ceil_div<int64_t>(m, kSumRows) * n * 4);
-  g.w = g.x + (g.laid ? m * row * size : 0);
-  g.parts = g.w + (g.laid ? n * row * size : 0);
-  const int64_t a = parts_bytes(m, k, n, slab, false), b = parts_bytes(n, k, m, slab, true);
-  g.total = g.parts + align16(a > b ? a : b);
-  return g;
-}
-
 template <typename T>
 hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
   const GradSpace g = grad_space(A.m, A.k, A.n, A.dtype, A.act);
@@ -1445,13 +1285,13 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
   const bool products = (A.dx || A.dw) && A.k > 0;
   if (A.m > 0 && A.n > 0 && ((g.dz_laid && products) || A.dbias)) {
     const int64_t strips = ceil_div<int64_t>(A.n, 512);
-    if (strips * chunks * 256 >= int64_t(1) << 32) return hipErrorInvalidConfiguration;
+    const int64_t places = strips * chunks;
     T *const to = g.dz_laid && products ? reinterpret_cast<T *>(ws + g.dz) : nullptr;
     float *const sums = A.dbias ? reinterpret_cast<float *>(ws + g.sums) : nullptr;
-    hipLaunchKernelGGL((k_dz<T>), dim3(unsigned(strips * chunks)), dim3(256), 0, stream,
+    hipLaunchKernelGGL((k_dz<T>), dim3(unsigned(std::min(places, kMostBlocks))), dim3(256), 0, stream,
                        static_cast<const T *>(A.dy), A.dy_stride,
                        has_act ? static_cast<const T *>(A.pre) : nullptr, A.pre_stride, A.act, A.m,
-                       A.n, strips, to, g.dz_stride, sums);
+                       A.n, strips, places, to, g.dz_stride, sums);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (to) {

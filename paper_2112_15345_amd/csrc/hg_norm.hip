@@ -499,18 +499,21 @@ __global__ __launch_bounds__(1024) void k_sum_parts(const float *__restrict__ pa
                                                     int64_t n, float *__restrict__ out) {
   __shared__ float red[32][33];
   const int col = threadIdx.x & 31, turn = threadIdx.x >> 5;
-  const int64_t j = int64_t(blockIdx.x) * 32 + col;
-  float s = 0.0f;
-  if (j < n) {
+  for (int64_t first = int64_t(blockIdx.x) * 32; first < n; first += int64_t(gridDim.x) * 32) {
+    const int64_t j = first + col;
+    float s = 0.0f;
+    if (j < n) {
 #pragma unroll 8
-    for (int64_t p = turn; p < parts; p += 32) s += part[p * n + j];
+      for (int64_t p = turn; p < parts; p += 32) s += part[p * n + j];
+    }
+    if (first != int64_t(blockIdx.x) * 32) __syncthreads();  // the last columns' have been read
+    red[turn][col] = s;
+    __syncthreads();
+    // (a wavefront now has two columns: their 32 sums, added in a fixed tree)
+    const float v = lanes_sum<32>(red[threadIdx.x & 31][threadIdx.x >> 5]);
+    const int64_t o = first + (threadIdx.x >> 5);
+    if ((threadIdx.x & 31) == 0 && o < n) out[o] = v;
   }
-  red[turn][col] = s;
-  __syncthreads();
-  // (a wavefront now has two columns: their 32 sums, added in a fixed tree)
-  const float v = lanes_sum<32>(red[threadIdx.x & 31][threadIdx.x >> 5]);
-  const int64_t o = int64_t(blockIdx.x) * 32 + (threadIdx.x >> 5);
-  if ((threadIdx.x & 31) == 0 && o < n) out[o] = v;
 }
 
 // How a row is shared: f.template run<G, NV>().
@@ -581,8 +584,9 @@ hipError_t forward(const hg_norm_args &A, hipStream_t stream) {
 hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n, float *out,
                             hipStream_t stream) {
   if (n <= 0) return hipSuccess;
-  hipLaunchKernelGGL(k_sum_parts, dim3(unsigned(ceil_div<int64_t>(n, 32))), dim3(1024), 0, stream,
-                     part, parts, n, out);
+  const int64_t blocks = std::min(ceil_div<int64_t>(n, 32), kMostBlocks);
+  hipLaunchKernelGGL(k_sum_parts, dim3(unsigned(blocks)), dim3(1024), 0, stream, part, parts, n,
+                     out);
   return hipGetLastError();
 }
 
