@@ -748,7 +748,7 @@ typedef struct hg_distill_args {
   int64_t rows, classes;      /* classes >= 1 */
   int32_t top;                /* 0 .. HG_MAX_TOP (HG_EUNSUPPORTED past it) */
   int32_t dtype, teacher_dtype;
-  float temperature;          /* > 0, finite */
+  float temperature;          /* > 0, finite (HG_EUNSUPPORTED below 2^-126) */
   const void *logits;         /* [rows, classes] */
   int64_t logits_stride;
   const int64_t *ids;         /* [rows, top] */

@@ -173,6 +173,9 @@ hg_status hg_distill(const hg_distill_args *a, hipStream_t stream) {
              a->teacher_dtype);
   HG_REQUIRE(a->temperature > 0.0f && std::isfinite(a->temperature),
              "hg_distill: the temperature is not positive and finite");
+  // (1 / temperature is not a float32 below)
+  if (a->temperature < 0x1p-126f)
+    return refuse(HG_EUNSUPPORTED, "hg_distill: a temperature below 2^-126");
   if (a->rows >= kMost || a->classes >= kMost)
     return refuse(HG_EUNSUPPORTED, "hg_distill: 2^31 rows or classes, or more");
   if (a->top > HG_MAX_TOP)
