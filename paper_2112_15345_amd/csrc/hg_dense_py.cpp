@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -67,6 +68,16 @@ const at::Tensor *given(PyObject *o, const char *name) {
   if (o == Py_None) return nullptr;
   if (!THPVariable_Check(o)) throw Unfit(std::string(name) + ": a tensor is wanted");
   return &THPVariable_Unpack(o);
+}
+
+// The forward calls record nothing for autograd: a gradient that torch would be asked for later is
+// refused here, not dropped.
+void no_gradient(std::initializer_list<PyObject *> tensors) {
+  if (!c10::GradMode::is_enabled()) return;
+  for (PyObject *o : tensors)
+    if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
+      throw Unfit("a tensor requires a gradient, and this call records none: call it under "
+                  "torch.no_grad(), or detach the tensor (the backward passes are calls of their own)");
 }
 
 void check_type(const at::Tensor &t, const char *name, Types types) {
@@ -213,6 +224,7 @@ int32_t code_or_none(const at::Tensor &t) {
 // rms_norm(x, weight, residual, ids, eps, out_dtype) -> (y, sum, scale)
 PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject * {
+    no_gradient({args[0], args[1], args[2]});
     const Taken t(args[0], args[3]);
     const at::Tensor &x = t.x;
     const auto dev = x.device();
@@ -297,6 +309,7 @@ PyObject *rms_norm_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
 // linear(x, w, bias, act, residual, x_scale, w_scale, out_dtype, keep_pre) -> (y, pre)
 PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> PyObject * {
+    no_gradient({args[0], args[1], args[2], args[4]});
     const at::Tensor x = matrix(args[0], "x", {at::kFloat, at::kHalf, at::kBFloat16,
                                                at::kFloat8_e4m3fn});
     const auto dev = x.device();
@@ -409,6 +422,8 @@ PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
 // distill(logits, ids, teacher, temperature, row_weight, want_loss, want_grad) -> (loss, grad)
 PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> PyObject * {
+    // (with the gradient asked for, logits may come from autograd: it goes back by logits.backward(grad))
+    if (!truth(args[6])) no_gradient({args[0]});
     const at::Tensor z = matrix(args[0], "logits", kFloats);
     const auto dev = z.device();
     const int64_t rows = z.size(0), classes = z.size(1);

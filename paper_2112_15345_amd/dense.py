@@ -7,6 +7,11 @@ a tensor whose columns are not contiguous is copied first.  Outputs and workspac
 are made on `stream` (default: the current stream), where the work runs; as with any
 torch call, tensors made on another stream have to be ready, and kept until it is done.
 
+Nothing is recorded for autograd: rms_norm, linear, and distill without its gradient refuse
+(ValueError) tensors that require one, unless gradients are off (torch.no_grad(), or the
+forward of a torch.autograd.Function).  The backward passes are calls of their own; distill's
+gradient can be given to logits.backward(grad).
+
     y, h, scale = rms_norm(x, weight, residual=r)            # h = x + r
     z, pre = linear(y, w, bias=b, act="gelu", residual=h, keep_pre=True)
     loss, grad = distill(logits, top_ids, top_logits, temperature=2.0, want_grad=True)
