@@ -75,7 +75,7 @@ const at::Tensor *given(PyObject *o, const char *name) {
 void no_gradient(std::initializer_list<PyObject *> tensors) {
   if (!c10::GradMode::is_enabled()) return;
   for (PyObject *o : tensors)
-    if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
+    if (o != Py_None && THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
       throw Unfit("a tensor requires a gradient, and this call records none: call it under "
                   "torch.no_grad(), or detach the tensor (the backward passes are calls of their own)");
 }
