@@ -72,7 +72,7 @@ hg_status hg_rms_norm(const hg_norm_args *a, hipStream_t stream) {
 
 int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim) {
   if (rows <= 0 || dim <= 0 || rows >= kMost || dim >= kMost) return 0;
-  return rms_norm_grad_parts(rows, dim) * dim * int64_t(sizeof(float));
+  return rms_norm_grad_parts(rows) * dim * int64_t(sizeof(float));
 }
 
 hg_status hg_rms_norm_grad(const hg_norm_grad_args *a, hipStream_t stream) {

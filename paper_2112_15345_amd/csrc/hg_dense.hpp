@@ -25,7 +25,7 @@ constexpr int64_t kMostBlocks = int64_t(1) << 20;
 
 hipError_t launch_rms_norm(const hg_norm_args &A, hipStream_t stream);
 hipError_t launch_rms_norm_grad(const hg_norm_grad_args &A, hipStream_t stream);
-int64_t rms_norm_grad_parts(int64_t rows, int64_t dim);
+int64_t rms_norm_grad_parts(int64_t rows);
 
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream);
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);

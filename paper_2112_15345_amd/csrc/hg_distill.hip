@@ -262,6 +262,7 @@ struct Row {
   __device__ __forceinline__ void listed_entries(T *grad, const Softmax &q) const {
     const RowLds L = at();
     const float f = a * inv_t / q.s;
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0f70);  // the sweep's stores are done (vmcnt 0)
     sync();
     if (nothing || a == 0.0f) return;

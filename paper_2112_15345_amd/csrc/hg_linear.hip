@@ -331,16 +331,6 @@ __device__ __forceinline__ void put(void *base, int64_t at, const float *v, int 
   for (int j = 0; j < N; ++j) t.e[j] = T(v[j]);
   t.template store<M>(static_cast<T *>(base) + at, n);
 }
-template <int N>
-__device__ __forceinline__ void put_as(void *base, int32_t dtype, int64_t at, const float *v,
-                                       int n) {
-  if (dtype == HG_DT_F32)
-    put<float, N>(base, at, v, n);
-  else if (dtype == HG_DT_F16)
-    put<_Float16, N>(base, at, v, n);
-  else
-    put<__bf16, N>(base, at, v, n);
-}
 template <typename T, int N>
 __device__ __forceinline__ void get(const void *base, int64_t at, float *v, int n) {
   Vec<T, N> t;

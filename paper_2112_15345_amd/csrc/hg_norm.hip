@@ -558,7 +558,7 @@ struct Backward {
   template <int G, int NV>
   hipError_t run() const {
     const int64_t blocks = ceil_div<int64_t>(A.rows, Group<G>::kRows);
-    const int64_t most = rms_norm_grad_parts(A.rows, A.dim);
+    const int64_t most = rms_norm_grad_parts(A.rows);
     const int64_t grid = blocks < most ? blocks : most;
     if constexpr (NV == 0)
       hipLaunchKernelGGL((k_rms_norm_grad_long<T>), dim3(unsigned(grid)), dim3(kBlock), 0, stream,
@@ -591,8 +591,7 @@ hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n, float *
 }
 
 // Parts of dweight: blocks of the backward pass, at most.
-int64_t rms_norm_grad_parts(int64_t rows, int64_t dim) {
-  (void)dim;
+int64_t rms_norm_grad_parts(int64_t rows) {
   return rows < kParts ? rows : kParts;
 }
 
