@@ -600,7 +600,8 @@ hg_status hg_bench_philox(uint64_t rng_seed, int32_t hop, int32_t etype, int64_t
  *   scale_i = max(max_j |y_j| / 448, 2^-126),  y8_j = e4m3(y_j / scale_i)
  * so that y8_j scale_i stands for y_j.  A NaN anywhere in a row makes the
  * row's y (and its scale) NaN; an infinity makes NaN at its own place (and
- * the scale NaN) and zeros elsewhere.
+ * the scale NaN) and zeros elsewhere.  The squares are summed in float32: a row
+ * whose sum passes its range (elements of some 1e19) comes out as zeros.
  * An id outside [0, x_rows) makes the row NaN (sum, y, scale): nothing is read
  * for it and nothing waits to report it.
  * sum may be x (without ids) or residual, y may be x (without ids) or
@@ -704,7 +705,8 @@ int64_t hg_linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);
  * pre: the forward call's (NULL with HG_ACT_NONE).  dx, dw (`dtype` or float32)
  * and dbias (float32) may each be NULL (not computed).  The residual's
  * gradient is dy.  relu's slope at 0 is 0.  With an activation, dz is rounded
- * to `dtype` before the two products (dbias sums it unrounded). */
+ * to `dtype` before the two products (dbias sums it unrounded); in float16 a dz
+ * past 65504 (slopes are up to 1.13) is an infinity there. */
 typedef struct hg_linear_grad_args {
   int64_t m, k, n;
   int32_t dtype, dw_dtype, act;

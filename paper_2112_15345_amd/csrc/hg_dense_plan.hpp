@@ -24,9 +24,10 @@ inline int64_t slab_of(int32_t dtype) { return dtype == HG_DT_F32 ? 32 : 64; }
 // How a product is cut: its tiles, how many slabs are in LDS, and the parts of its depth.
 // A compute unit that multiplies one tile waits for its loads unless several slabs are in
 // flight; with two tiles each covers the other's waits.
-//  kLarge   256 x 256, 2 slabs, one block on a unit: 1.28 PF/s in 16 bits at 8192^3.  Not
-//           for depths below 8 slabs (150001 x 128 x 256: 36 us, kMedium 33) nor in 32 bits,
-//           whose products take too long for its uneven last round
+//  kLarge   256 x 256, 2 slabs, one block on a unit: 1.24 to 1.28 PF/s in 16 bits at 8192^3.
+//           From depths of 8 slabs on (32768 rows, 2048 columns, by depth: 128 49 us, kMedium
+//           45; 256 60, 57; 512 84, 84; 1024 133, 141), and not in 32 bits, whose products
+//           take too long for its uneven last round
 //  kMedium  128 x 128, 2 slabs, two blocks: loading a slab takes as long as multiplying it
 //           (64 bytes a clock), 1.0 PF/s at 8192^3, but its tiles fill the units better
 //  kSmall   64 x 64, 4 slabs, two blocks: for too few tiles of the others (1024^3: 8.8 us,
@@ -34,6 +35,13 @@ inline int64_t slab_of(int32_t dtype) { return dtype == HG_DT_F32 ? 32 : 64; }
 //           columns' gradient over 65537 rows: 172 us, kMedium 112)
 //  kTall    256 x 128 in slabs of 64 bytes, two blocks: the weight gradients' operands,
 //           whose slabs are read across (8192^3: 1.20 PF/s, kLarge 1.11, kMedium 1.04)
+// kLarge needs two rounds of tiles: with fewer, what counts is how full the last one is, which
+// the rule does not look at (us, kLarge / kMedium, tiles of 256 x 256: 16384 x 4096 x 1024, 256
+// tiles, 119 / 138; 12288 x 1024 x 2048, 384, 65 / 54; 16384 x 2048 x 1792, 448, 112 / 128;
+// 8192 x 4096 x 4096, 512, 224 / 262; 12288 x 2048 x 3328, 624, 167 / 160).  kTall needs half a
+// round of its tiles (gradients of n x k weights over m rows, m x k x n, kTall / without:
+// 16384 x 2048 x 4096, 256 tiles, 295 / 313; 16385 x 1024 x 4096, 128, 168 / 175; 8192 x 2048 x
+// 2048, 128, 87 / 86; 65537 x 512 x 1024, 16, 120 / 109).
 enum class Cut { kLarge, kMedium, kSmall, kTall };
 struct Plan {
   Cut cut;
@@ -95,7 +103,10 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, boo
       }
     } else if (tiles <= 6 * at_once && filled(tiles, at_once) < 0.9 && depth >= 16 * slab) {
       // the rows of whole rounds; the last round's few tiles would leave most units idle
-      // for as long as a full one takes, and are cut finer
+      // for as long as a full one takes, and are cut finer (us, cut / not: 25000 x 1024 x 2048,
+      // rounds filled by 0.77, 110 / 124; 28000 x 2048 x 2048, 0.86, 220 / 228; 30000 x 1024 x
+      // 2048, 0.92, 142 / 128; by depth, 0.80: 65537 x 1024 x 1024 137 / 145, and with 8 slabs
+      // 65537 x 512 x 1024 82 / 85, but 137 / 133 with residual and pre)
       const int64_t down = tiles / at_once * at_once / ceil_div<int64_t>(cols, p.tile_j);
       if (down > 0) p.rows = down * p.tile_i;
     }

@@ -997,7 +997,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
 // ---- dz and its column sums ------------------------------------------------------
 
 // dz = dy act'(pre) in T (dz NULL: not written), zeros from column n to its stride, and the
-// sums over the block's rows.
+// sums over the block's rows.  In T, because the products' instructions take 16-bit operands: the
+// bits that go (the error of dx and dw against 64 bits is 0.0023 for it, 0.0017 without, of their
+// sizes in bfloat16) would be a second piece of dz, and twice the time of both products.
 // A wavefront takes 64 vectors of 8 columns; the block's four take turns over the rows.
 // Place b: columns b % strips, rows b / strips; a block takes every gridDim.x-th place.
 template <typename T>
