@@ -56,7 +56,8 @@ typedef enum hg_dtype {
   HG_DT_F32 = 1,
   HG_DT_F16 = 2,
   HG_DT_BF16 = 3,
-  HG_DT_E4M3 = 4
+  HG_DT_E4M3 = 4,
+  HG_DT_I8 = 6
 } hg_dtype;
 
 /* One node type (Sec. 4.1.4: features are stored per node type, in an ID
@@ -654,6 +655,70 @@ typedef struct hg_norm_grad_args {
 } hg_norm_grad_args;
 hg_status hg_rms_norm_grad(const hg_norm_grad_args *args, hipStream_t stream);
 int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim);
+
+/* Layer norm with the residual's addition.  For row i < rows:
+ *   h = x[i] + residual[i]  (x[ids[i]] with ids; no residual: h = x)
+ *   d = h - mean_j h_j,  s = 1 / sqrt(mean_j d_j^2 + eps),  y_j = d_j s weight_j + bias_j
+ * sum (NULL: not written) receives h in `dtype`; the norm is of the unrounded h.
+ * y in `dtype`; or in 8 bits with a scale per row, so that y8_j scale_i stands for y_j:
+ *   out_dtype HG_DT_E4M3   scale_i = max(max_j |y_j| / 448, 2^-126),  y8_j = e4m3(y_j / scale_i)
+ *   out_dtype HG_DT_I8     scale_i = max(max_j |y_j| / 127, 2^-126),  y8_j = y_j / scale_i,
+ *                          rounded to the nearest integer (of two as near, the even one)
+ * The mean is taken first and the squares are summed around it, in float32.  A NaN or an infinity
+ * anywhere in a row, or a sum past float32's range, makes its y NaN (and its scale); in 8-bit
+ * integers, which have no NaN, the row is zeros and its scale NaN.  An id outside [0, x_rows) makes
+ * the row such a row: nothing is read for it and nothing waits to report it.  With eps 0 a row
+ * of equal elements has no y: it is NaN, or what rounding makes of it.
+ * sum may be x (without ids) or residual, y may be x (without ids) or residual (in `dtype`),
+ * each with the same stride. */
+typedef struct hg_layer_norm_args {
+  int64_t rows, dim;          /* dim >= 1 */
+  int32_t dtype, out_dtype;   /* out_dtype: dtype, HG_DT_E4M3 or HG_DT_I8 */
+  int32_t weight_dtype;       /* HG_DT_F32 or dtype; HG_DT_NONE: no weight (1) */
+  int32_t bias_dtype;         /* HG_DT_F32 or dtype; HG_DT_NONE: no bias (0) */
+  float eps;                  /* >= 0 */
+  const void *x;
+  int64_t x_stride, x_rows;   /* x_rows: rows of x, read with ids only */
+  const int64_t *ids;         /* [rows] or NULL */
+  const void *residual;       /* [rows, dim] or NULL */
+  int64_t residual_stride;
+  const void *weight, *bias;  /* [dim] */
+  void *y;
+  int64_t y_stride;
+  float *scale;               /* [rows], with 8-bit results */
+  void *sum;
+  int64_t sum_stride;
+} hg_layer_norm_args;
+hg_status hg_layer_norm(const hg_layer_norm_args *args, hipStream_t stream);
+
+/* The backward pass of hg_layer_norm, from the rows that were normalised (x: the forward call's
+ * sum, or its x with the same ids when it had no residual), the gradient dy of y and the gradient
+ * dsum of sum (NULL: none):
+ *   g = dy weight,  n = d s,  dx = s (g - mean(g) - n mean(g n)) + dsum,
+ *   dweight_j = sum_i dy_ij n_ij,  dbias_j = sum_i dy_ij
+ * dx is the gradient of both x and residual (row i belongs to x[ids[i]]); dx, dweight and dbias may
+ * each be NULL (not computed).  An 8-bit y counts as unrounded.  dx may be dy or dsum or (without
+ * ids) x, with the same stride.  dweight and dbias are summed over the rows in a fixed order. */
+typedef struct hg_layer_norm_grad_args {
+  int64_t rows, dim;
+  int32_t dtype, weight_dtype;
+  float eps;
+  const void *x;
+  int64_t x_stride, x_rows;
+  const int64_t *ids;
+  const void *weight;
+  const void *dy;
+  int64_t dy_stride;
+  const void *dsum;
+  int64_t dsum_stride;
+  void *dx;
+  int64_t dx_stride;
+  float *dweight, *dbias;     /* [dim] float32; zeros when rows == 0 */
+  void *workspace;            /* for dweight or dbias */
+  int64_t workspace_bytes;
+} hg_layer_norm_grad_args;
+hg_status hg_layer_norm_grad(const hg_layer_norm_grad_args *args, hipStream_t stream);
+int64_t hg_layer_norm_grad_workspace(int64_t rows, int64_t dim);
 
 /* Matrix product with bias, activation and residual in one pass:
  *   z = x w^T + bias,  y = act(z) + residual

@@ -16,7 +16,7 @@ is not built; there is no CPU path.
     indptr, src_local, dst_local, eid = b.edges(hop, etype)
     x = g.gather_features(b, ntype)
 
-The dense operators that a model runs on such rows (rms_norm, linear, distill and
+The dense operators that a model runs on such rows (rms_norm, layer_norm, linear, distill and
 their backward passes) are in `dense`, and under this package's name.
 """
 from __future__ import annotations
@@ -59,7 +59,7 @@ ABI_SYMBOLS = ("hg_create", "hg_destroy", "hg_retire_stream", "hg_sample_blocks"
                "hg_gather_rows_noalloc",
                "hg_rms_norm", "hg_rms_norm_grad", "hg_rms_norm_grad_workspace",
                "hg_linear", "hg_linear_workspace", "hg_linear_grad", "hg_linear_grad_workspace",
-               "hg_distill")
+               "hg_distill", "hg_layer_norm", "hg_layer_norm_grad", "hg_layer_norm_grad_workspace")
 
 HG_MAX_NEG = 64
 HG_MAX_TIMED_HOPS = 8
@@ -165,6 +165,9 @@ def _bind(lib: ctypes.CDLL) -> ctypes.CDLL:
         "hg_linear_grad": ([_P, _P], _I32),
         "hg_linear_grad_workspace": ([_I64, _I64, _I64, _I32, _I32], _I64),
         "hg_distill": ([_P, _P], _I32),
+        "hg_layer_norm": ([_P, _P], _I32),
+        "hg_layer_norm_grad": ([_P, _P], _I32),
+        "hg_layer_norm_grad_workspace": ([_I64, _I64], _I64),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -209,7 +212,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         dense.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.hg_rms_norm, lib.hg_rms_norm_grad, lib.hg_rms_norm_grad_workspace, lib.hg_linear,
             lib.hg_linear_workspace, lib.hg_linear_grad, lib.hg_linear_grad_workspace,
-            lib.hg_distill)))
+            lib.hg_distill, lib.hg_layer_norm, lib.hg_layer_norm_grad,
+            lib.hg_layer_norm_grad_workspace)))
         _views, _dense = views, dense
         _lib = lib
     return _lib
@@ -953,5 +957,5 @@ def bench_philox(rng_seed: int, hop: int, etype: int, n_groups: int, lim: int,
 
 
 from .dense import (HG_ACT_GELU, HG_ACT_NONE, HG_ACT_RELU, HG_ACT_SILU,  # noqa: E402,F401
-                    HG_DT_E4M3, HG_MAX_TOP, distill, linear, linear_grad, rms_norm,
-                    rms_norm_grad)
+                    HG_DT_E4M3, HG_DT_I8, HG_MAX_TOP, distill, layer_norm, layer_norm_grad, linear,
+                    linear_grad, rms_norm, rms_norm_grad)

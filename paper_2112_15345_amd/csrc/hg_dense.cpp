@@ -23,6 +23,12 @@ constexpr int64_t kMost = int64_t(1) << 31;
 
 bool is_float(int32_t dt) { return dt == HG_DT_F32 || dt == HG_DT_F16 || dt == HG_DT_BF16; }
 
+bool is_8_bits(int32_t dt) { return dt == HG_DT_E4M3 || dt == HG_DT_I8; }
+// The type of a weight or bias over columns of `dtype`.
+bool columns_ok(int32_t dt, int32_t dtype) {
+  return dt == HG_DT_NONE || dt == HG_DT_F32 || dt == dtype;
+}
+
 #define HG_REQUIRE(cond, ...) \
   do {                        \
     if (!(cond)) return refuse(HG_EINVAL, __VA_ARGS__); \
@@ -100,6 +106,63 @@ hg_status hg_rms_norm_grad(const hg_norm_grad_args *a, hipStream_t stream) {
   }
   clear_pending();
   return launched(launch_rms_norm_grad(*a, stream), "hg_rms_norm_grad");
+}
+
+hg_status hg_layer_norm(const hg_layer_norm_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_layer_norm: NULL arguments");
+  HG_REQUIRE(a->rows >= 0 && a->dim >= 1, "hg_layer_norm: rows < 0 or dim < 1");
+  HG_REQUIRE(is_float(a->dtype), "hg_layer_norm: type %d", a->dtype);
+  HG_REQUIRE(a->out_dtype == a->dtype || is_8_bits(a->out_dtype), "hg_layer_norm: output type %d",
+             a->out_dtype);
+  HG_REQUIRE(columns_ok(a->weight_dtype, a->dtype), "hg_layer_norm: weight type %d",
+             a->weight_dtype);
+  HG_REQUIRE(columns_ok(a->bias_dtype, a->dtype), "hg_layer_norm: bias type %d", a->bias_dtype);
+  HG_REQUIRE(a->eps >= 0.0f && std::isfinite(a->eps),
+             "hg_layer_norm: eps is negative or not finite");
+  if (a->rows >= kMost || a->dim >= kMost)
+    return refuse(HG_EUNSUPPORTED, "hg_layer_norm: 2^31 rows or columns, or more");
+  if (a->rows == 0) return HG_OK;
+  HG_REQUIRE(in_ok(a->x, a->x_stride), "hg_layer_norm: x is NULL or its stride negative");
+  HG_REQUIRE(!a->ids || a->x_rows >= 0, "hg_layer_norm: x_rows < 0");
+  HG_REQUIRE(!a->residual || a->residual_stride >= 0, "hg_layer_norm: residual stride");
+  HG_REQUIRE(a->weight_dtype == HG_DT_NONE || a->weight, "hg_layer_norm: weight is NULL");
+  HG_REQUIRE(a->bias_dtype == HG_DT_NONE || a->bias, "hg_layer_norm: bias is NULL");
+  HG_REQUIRE(out_ok(a->y, a->y_stride, a->dim), "hg_layer_norm: y is NULL or its stride below dim");
+  HG_REQUIRE(!a->sum || a->sum_stride >= a->dim, "hg_layer_norm: sum's stride below dim");
+  HG_REQUIRE(!is_8_bits(a->out_dtype) || a->scale, "hg_layer_norm: 8 bits need scale");
+  clear_pending();
+  return launched(launch_layer_norm(*a, stream), "hg_layer_norm");
+}
+
+int64_t hg_layer_norm_grad_workspace(int64_t rows, int64_t dim) {
+  return 2 * hg_rms_norm_grad_workspace(rows, dim);
+}
+
+hg_status hg_layer_norm_grad(const hg_layer_norm_grad_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_layer_norm_grad: NULL arguments");
+  HG_REQUIRE(a->rows >= 0 && a->dim >= 1, "hg_layer_norm_grad: rows < 0 or dim < 1");
+  HG_REQUIRE(is_float(a->dtype), "hg_layer_norm_grad: type %d", a->dtype);
+  HG_REQUIRE(columns_ok(a->weight_dtype, a->dtype), "hg_layer_norm_grad: weight type %d",
+             a->weight_dtype);
+  HG_REQUIRE(a->eps >= 0.0f && std::isfinite(a->eps),
+             "hg_layer_norm_grad: eps is negative or not finite");
+  if (a->rows >= kMost || a->dim >= kMost)
+    return refuse(HG_EUNSUPPORTED, "hg_layer_norm_grad: 2^31 rows or columns, or more");
+  if (!a->dx && !a->dweight && !a->dbias) return HG_OK;
+  if (a->rows > 0) {
+    HG_REQUIRE(in_ok(a->x, a->x_stride), "hg_layer_norm_grad: x is NULL or its stride negative");
+    HG_REQUIRE(!a->ids || a->x_rows >= 0, "hg_layer_norm_grad: x_rows < 0");
+    HG_REQUIRE(in_ok(a->dy, a->dy_stride), "hg_layer_norm_grad: dy is NULL or its stride negative");
+    HG_REQUIRE(!a->dsum || a->dsum_stride >= 0, "hg_layer_norm_grad: dsum stride");
+    HG_REQUIRE(a->weight_dtype == HG_DT_NONE || a->weight, "hg_layer_norm_grad: weight is NULL");
+    HG_REQUIRE(!a->dx || a->dx_stride >= a->dim, "hg_layer_norm_grad: dx stride below dim");
+    HG_REQUIRE((!a->dweight && !a->dbias) ||
+                   (a->workspace &&
+                    a->workspace_bytes >= hg_layer_norm_grad_workspace(a->rows, a->dim)),
+               "hg_layer_norm_grad: workspace too small");
+  }
+  clear_pending();
+  return launched(launch_layer_norm_grad(*a, stream), "hg_layer_norm_grad");
 }
 
 int64_t hg_linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {

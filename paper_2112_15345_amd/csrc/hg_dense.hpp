@@ -1,5 +1,5 @@
-// Shared by the dense operators (hg_norm.hip, hg_linear.hip, hg_distill.hip) and
-// their C entry points (hg_dense.cpp): element types, vector loads and stores,
+// Shared by the dense operators (hg_norm.hip, hg_layer_norm.hip, hg_linear.hip, hg_distill.hip,
+// hg_embed.hip, hg_quantize.hip) and their C entry points (hg_dense.cpp): element types, vector loads and stores,
 // reductions, and the launchers.
 #pragma once
 
@@ -27,6 +27,9 @@ hipError_t launch_rms_norm(const hg_norm_args &A, hipStream_t stream);
 hipError_t launch_rms_norm_grad(const hg_norm_grad_args &A, hipStream_t stream);
 int64_t rms_norm_grad_parts(int64_t rows);
 
+hipError_t launch_layer_norm(const hg_layer_norm_args &A, hipStream_t stream);
+hipError_t launch_layer_norm_grad(const hg_layer_norm_grad_args &A, hipStream_t stream);
+
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream);
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);
 hipError_t launch_linear_grad(const hg_linear_grad_args &A, hipStream_t stream);
@@ -37,6 +40,9 @@ hipError_t launch_distill(const hg_distill_args &A, hipStream_t stream);
 // out[j] = sum over p < parts of part[p * n + j], in the order of p.
 hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n, float *out,
                             hipStream_t stream);
+// The same of n1 + n2 columns, the first n1 to out and the others to out2.
+hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n1, float *out, int64_t n2,
+                            float *out2, hipStream_t stream);
 
 // ---- device helpers ----------------------------------------------------------
 

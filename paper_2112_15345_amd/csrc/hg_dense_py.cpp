@@ -17,6 +17,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 #include <initializer_list>
 #include <optional>
 #include <string>
@@ -34,7 +35,11 @@ struct Api {
   decltype(&hg_linear_grad) linear_grad = nullptr;
   decltype(&hg_linear_grad_workspace) linear_grad_workspace = nullptr;
   decltype(&hg_distill) distill = nullptr;
+  decltype(&hg_layer_norm) layer_norm = nullptr;
+  decltype(&hg_layer_norm_grad) layer_norm_grad = nullptr;
+  decltype(&hg_layer_norm_grad_workspace) layer_norm_grad_workspace = nullptr;
 } api;
+constexpr int kEntries = int(sizeof(Api) / sizeof(void *));
 
 // An argument that does not fit: ValueError.
 struct Unfit : std::exception {
@@ -60,6 +65,7 @@ int32_t code_of(at::ScalarType t) {
     case at::kHalf: return HG_DT_F16;
     case at::kBFloat16: return HG_DT_BF16;
     case at::kFloat8_e4m3fn: return HG_DT_E4M3;
+    case at::kChar: return HG_DT_I8;
     default: return HG_DT_NONE;
   }
 }
@@ -212,9 +218,9 @@ struct Taken {
     rows = ids.defined() ? ids.size(0) : x.size(0);
   }
 };
-at::Tensor norm_weight(PyObject *o, const at::Tensor &x) {
+at::Tensor norm_weight(PyObject *o, const at::Tensor &x, const char *name = "weight") {
   return optional(o, [&](PyObject *w) {
-    return vector(w, "weight", {at::kFloat, x.scalar_type()}, x.device(), x.size(1));
+    return vector(w, name, {at::kFloat, x.scalar_type()}, x.device(), x.size(1));
   });
 }
 int32_t code_or_none(const at::Tensor &t) {
@@ -303,6 +309,99 @@ PyObject *rms_norm_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     a.workspace = ptr(ws);
     a.workspace_bytes = bytes_of(ws);
     return result(api.rms_norm_grad(&a, current_stream(dev)), {dx, dw});
+  });
+}
+
+// layer_norm(x, weight, bias, residual, ids, eps, out_dtype) -> (y, sum, scale)
+PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject * {
+    no_gradient({args[0], args[1], args[2], args[3]});
+    const Taken t(args[0], args[4]);
+    const at::Tensor &x = t.x;
+    const auto dev = x.device();
+    const auto type = x.scalar_type();
+    const int64_t rows = t.rows, dim = x.size(1);
+    const at::Tensor w = norm_weight(args[1], x), b = norm_weight(args[2], x, "bias");
+    const at::Tensor r = optional(args[3], [&](PyObject *o) {
+      return matrix(o, "residual", {type}, dev, rows, dim);
+    });
+    const auto out = type_or(args[6], type, "out_dtype");
+    const bool eight = out == at::kFloat8_e4m3fn || out == at::kChar;
+    if (out != type && !eight)
+      throw Unfit("out_dtype: none of x's, torch.float8_e4m3fn, torch.int8");
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor y = make({rows, dim}, out, dev);
+    const at::Tensor sum = r.defined() ? make({rows, dim}, type, dev) : at::Tensor();
+    const at::Tensor scale = eight ? make({rows}, at::kFloat, dev) : at::Tensor();
+    hg_layer_norm_args a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = code_of(type);
+    a.out_dtype = code_of(out);
+    a.weight_dtype = code_or_none(w);
+    a.bias_dtype = code_or_none(b);
+    a.eps = float(number(args[5]));
+    a.x = ptr(x);
+    a.x_stride = stride(x);
+    a.x_rows = x.size(0);
+    a.ids = static_cast<const int64_t *>(ptr(t.ids));
+    a.residual = ptr(r);
+    a.residual_stride = stride(r);
+    a.weight = ptr(w);
+    a.bias = ptr(b);
+    a.y = ptr(y);
+    a.y_stride = dim;
+    a.scale = static_cast<float *>(ptr(scale));
+    a.sum = ptr(sum);
+    a.sum_stride = dim;
+    return result(api.layer_norm(&a, current_stream(dev)), {y, sum, scale});
+  });
+}
+
+// layer_norm_grad(dy, x, weight, dsum, ids, eps, want_dx, want_dweight or None, want_dbias)
+//   -> (dx, dweight, dbias)
+PyObject *layer_norm_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject * {
+    const Taken t(args[1], args[4]);
+    const at::Tensor &x = t.x;
+    const auto dev = x.device();
+    const auto type = x.scalar_type();
+    const int64_t rows = t.rows, dim = x.size(1);
+    const at::Tensor dy = matrix(args[0], "dy", {type}, dev, rows, dim);
+    const at::Tensor ds = optional(args[3], [&](PyObject *o) {
+      return matrix(o, "dsum", {type}, dev, rows, dim);
+    });
+    const at::Tensor w = norm_weight(args[2], x);
+    const bool want_dw = args[7] == Py_None ? w.defined() : truth(args[7]);
+    const bool want_db = truth(args[8]);
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor dx = truth(args[6]) ? make({rows, dim}, type, dev) : at::Tensor();
+    const at::Tensor dw = want_dw ? make({dim}, at::kFloat, dev) : at::Tensor();
+    const at::Tensor db = want_db ? make({dim}, at::kFloat, dev) : at::Tensor();
+    const at::Tensor ws =
+        workspace(want_dw || want_db ? api.layer_norm_grad_workspace(rows, dim) : 0, dev);
+    hg_layer_norm_grad_args a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = code_of(type);
+    a.weight_dtype = code_or_none(w);
+    a.eps = float(number(args[5]));
+    a.x = ptr(x);
+    a.x_stride = stride(x);
+    a.x_rows = x.size(0);
+    a.ids = static_cast<const int64_t *>(ptr(t.ids));
+    a.weight = ptr(w);
+    a.dy = ptr(dy);
+    a.dy_stride = stride(dy);
+    a.dsum = ptr(ds);
+    a.dsum_stride = stride(ds);
+    a.dx = ptr(dx);
+    a.dx_stride = dim;
+    a.dweight = static_cast<float *>(ptr(dw));
+    a.dbias = static_cast<float *>(ptr(db));
+    a.workspace = ptr(ws);
+    a.workspace_bytes = bytes_of(ws);
+    return result(api.layer_norm_grad(&a, current_stream(dev)), {dx, dw, db});
   });
 }
 
@@ -460,23 +559,17 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 // bind(addresses of the entry points, in Api's order)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  if (n != 8) {
-    PyErr_SetString(PyExc_TypeError, "bind() takes eight addresses");
+  if (n != kEntries) {
+    PyErr_Format(PyExc_TypeError, "bind() takes %d addresses", kEntries);
     return nullptr;
   }
-  int64_t v[8];
-  for (int i = 0; i < 8; ++i) {
-    v[i] = PyLong_AsLongLong(args[i]);
-    if (v[i] == -1 && PyErr_Occurred()) return nullptr;
+  void *v[kEntries];
+  for (int i = 0; i < kEntries; ++i) {
+    v[i] = PyLong_AsVoidPtr(args[i]);
+    if (!v[i] && PyErr_Occurred()) return nullptr;
   }
-  api.rms_norm = reinterpret_cast<decltype(api.rms_norm)>(v[0]);
-  api.rms_norm_grad = reinterpret_cast<decltype(api.rms_norm_grad)>(v[1]);
-  api.rms_norm_grad_workspace = reinterpret_cast<decltype(api.rms_norm_grad_workspace)>(v[2]);
-  api.linear = reinterpret_cast<decltype(api.linear)>(v[3]);
-  api.linear_workspace = reinterpret_cast<decltype(api.linear_workspace)>(v[4]);
-  api.linear_grad = reinterpret_cast<decltype(api.linear_grad)>(v[5]);
-  api.linear_grad_workspace = reinterpret_cast<decltype(api.linear_grad_workspace)>(v[6]);
-  api.distill = reinterpret_cast<decltype(api.distill)>(v[7]);
+  static_assert(sizeof(v) == sizeof(api));
+  std::memcpy(static_cast<void *>(&api), v, sizeof(v));
   Py_RETURN_NONE;
 }
 
@@ -489,6 +582,8 @@ PyMethodDef method(const char *name) {
 PyMethodDef methods[] = {method<bind>("bind"),
                          method<rms_norm>("rms_norm"),
                          method<rms_norm_grad>("rms_norm_grad"),
+                         method<layer_norm>("layer_norm"),
+                         method<layer_norm_grad>("layer_norm_grad"),
                          method<linear>("linear"),
                          method<linear_grad>("linear_grad"),
                          method<distill>("distill"),

@@ -6,153 +6,10 @@
 // Bound by memory: a row is read once, kept in registers, reduced, and written
 // once.  A group of 8 to 64 lanes, or a block, takes a row; each lane holds up to
 // kMaxVecs vectors of 16 bytes of it.  Rows longer than that are read twice.
-#include "hg_dense.hpp"
+#include "hg_rows.hpp"
 
 namespace hg {
 namespace {
-
-constexpr int kBlock = 256;
-// Blocks of a walk over the rows: 8 on each of 256 compute units going forward; fewer
-// going backward, where each leaves a part of dweight.
-constexpr int64_t kResident = 2048;
-constexpr int64_t kParts = 1024;
-
-// Threads that share a row, and how to reduce over them.  Past a wavefront each
-// reduction goes through one of two LDS buffers in turn, so that one barrier is enough.
-template <int G>
-struct Group {
-  static constexpr int kRows = kBlock / G;  // rows of a block at a time
-  static constexpr int kLds = G > 64 ? 4 * (kBlock / 64) : 1;
-  float *red;  // LDS [kLds]
-  int turn = 0;
-  __device__ explicit Group(float *lds) : red(lds) {}
-  // Sums of two values.
-  __device__ __forceinline__ void sum(float &a, float &b) {
-    a = lanes_sum<(G < 64 ? G : 64)>(a);
-    b = lanes_sum<(G < 64 ? G : 64)>(b);
-    if (G > 64) {
-      float *const r = red + (turn ^= 1) * 2 * (kBlock / 64);
-      if ((threadIdx.x & 63) == 0) {
-        r[threadIdx.x >> 6] = a;
-        r[kBlock / 64 + (threadIdx.x >> 6)] = b;
-      }
-      __syncthreads();
-      a = b = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kBlock / 64; ++i) {
-        a += r[i];
-        b += r[kBlock / 64 + i];
-      }
-    }
-  }
-  __device__ __forceinline__ float sum(float v) {
-    float none = 0.0f;
-    sum(v, none);
-    return v;
-  }
-  __device__ __forceinline__ uint32_t max(uint32_t v) {
-    v = lanes_max_bits<(G < 64 ? G : 64)>(v);
-    if (G > 64) {
-      float *const r = red + (turn ^= 1) * 2 * (kBlock / 64);
-      if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = __uint_as_float(v);
-      __syncthreads();
-      v = 0;
-#pragma unroll
-      for (int i = 0; i < kBlock / 64; ++i) v = ::max(v, __float_as_uint(r[i]));
-    }
-    return v;
-  }
-};
-
-// The largest magnitude as bits: NaN is above infinity, so it is kept.
-__device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
-__device__ __forceinline__ float scale_of(uint32_t amax) {
-  const float a = __uint_as_float(amax);
-  // (not fmax: it would drop a NaN)
-  const float c = a / 448.0f;
-  return c < 0x1p-126f ? 0x1p-126f : c;
-}
-
-// Four values in 8 bits, rounded to nearest even; |v| <= 448 or NaN.
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
-}
-
-template <int V>
-__device__ __forceinline__ void store_e4m3(uint8_t *p, const float *v, int n) {
-  uint32_t w[V / 4];
-#pragma unroll
-  for (int i = 0; i < V / 4; ++i)
-    w[i] = pack_e4m3(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-  if (n >= V) {
-    __builtin_memcpy(p, w, V);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < n) p[i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void load_weight(const hg_norm_args &A, int64_t c, int n, float *w) {
-  constexpr int V = kVec<T>;
-  if (A.weight_dtype == HG_DT_NONE) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = 1.0f;
-  } else if (A.weight_dtype == HG_DT_F32) {
-    Vec<float, V> t;
-    t.load(static_cast<const float *>(A.weight) + c, n);
-#pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = t.e[i];
-  } else {
-    Vec<T> t;
-    t.load(static_cast<const T *>(A.weight) + c, n);
-#pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = float(t.e[i]);
-  }
-}
-
-// The row that position i stands for: its place in x, or -1 where the id is out of
-// range.
-struct Source {
-  const int64_t *ids;
-  int64_t rows;
-  __device__ __forceinline__ int64_t at(int64_t i) const {
-    if (!ids) return i;
-    const int64_t v = ids[i];
-    return v >= 0 && v < rows ? v : -1;
-  }
-};
-
-template <typename T>
-__device__ __forceinline__ void fill_nan(Vec<T> &t) {
-#pragma unroll
-  for (int j = 0; j < kVec<T>; ++j) t.e[j] = T(__builtin_nanf(""));
-}
-
-// One vector (n > 0 elements of it) of a row of x; its elements past n are 0.
-template <typename T, Move M = Move::kStreamed>
-__device__ __forceinline__ void load_x(const void *x, int64_t stride, int64_t at, int c, int n,
-                                       Vec<T> &t) {
-  if (at >= 0) {
-    t.template load<M>(static_cast<const T *>(x) + at * stride + c, n);
-  } else {
-    fill_nan(t);
-#pragma unroll
-    for (int j = 0; j < kVec<T>; ++j)
-      if (j >= n) t.e[j] = T(0.0f);
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void store_row(T *p, const float *v, int n) {
-  Vec<T> t;
-#pragma unroll
-  for (int j = 0; j < kVec<T>; ++j) t.e[j] = T(v[j]);
-  t.template store<Move::kStreamed>(p, n);
-}
 
 // NV vectors a lane hold the row (NV > 0).  Groups walk over the rows and load the next
 // one while this one is reduced and written.
@@ -174,7 +31,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm(hg_norm_args A) {
     const int c = (v * G + lane) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j) w[v][j] = 0.0f;
-    if (c < dim) load_weight<T>(A, c, dim - c, w[v]);
+    if (c < dim) load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, dim - c, w[v]);
   }
   Vec<T> x[NV], r[NV];
   auto load = [&](int64_t row, int64_t at) {
@@ -284,7 +141,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
       for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
         float h[V], w[V];
         load_h(c, h);
-        load_weight<T>(A, c, dim - c, w);
+        load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, dim - c, w);
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (j < dim - c) amax = max(amax, mag(h[j] * s * w[j]));
@@ -298,7 +155,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_long(hg_norm_args A) {
       const int n = dim - c;
       float h[V], w[V];
       load_h(c, h);
-      load_weight<T>(A, c, n, w);
+      load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, n, w);
       if (A.sum) store_row<T>(static_cast<T *>(A.sum) + i * A.sum_stride + c, h, n);
 #pragma unroll
       for (int j = 0; j < V; ++j) h[j] = h[j] * s * w[j] * f;
@@ -325,16 +182,13 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad(hg_norm_grad_args A) {
   const float inv = 1.0f / float(dim);
   const Source src{A.ids, A.x_rows};
   const int64_t step = int64_t(gridDim.x) * kRows;
-  hg_norm_args N{};  // the forward's view of the weight
-  N.weight = A.weight;
-  N.weight_dtype = A.weight_dtype;
   float dw[NV][V], w[NV][V];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = (v * G + lane) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j) dw[v][j] = w[v][j] = 0.0f;
-    if (c < dim) load_weight<T>(N, c, dim - c, w[v]);
+    if (c < dim) load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, dim - c, w[v]);
   }
   Vec<T> x[NV], d[NV];
 #pragma unroll
@@ -438,9 +292,6 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
   Group<kBlock> grp(red);
   const uint32_t dim = uint32_t(A.dim);
   const Source src{A.ids, A.x_rows};
-  hg_norm_args N{};
-  N.weight = A.weight;
-  N.weight_dtype = A.weight_dtype;
   float *const part =
       A.dweight ? static_cast<float *>(A.workspace) + int64_t(blockIdx.x) * dim : nullptr;
   if (part)
@@ -455,7 +306,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
       Vec<T> d, x;
       d.load(dy + c, dim - c);
       load_x<T, Move::kCached>(A.x, A.x_stride, at, c, dim - c, x);
-      load_weight<T>(N, c, dim - c, w);
+      load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, dim - c, w);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float h = float(x.e[j]);
@@ -473,7 +324,7 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
       Vec<T> d, x;
       d.load(dy + c, n);
       load_x<T, Move::kCached>(A.x, A.x_stride, at, c, n, x);
-      load_weight<T>(N, c, n, w);
+      load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, n, w);
       if (part)
         for (int j = 0; j < V && j < n; ++j)
           part[c + j] += float(d.e[j]) * (float(x.e[j]) * s);
@@ -495,8 +346,10 @@ __global__ __launch_bounds__(kBlock) void k_rms_norm_grad_long(hg_norm_grad_args
 // 32 columns a block, 32 threads for each, which take turns over the parts and are
 // added in LDS: a thread then has few loads that follow each other (1024 parts, 128
 // columns: 4 us, where 4 threads for a column took 65).
+// Columns from n1 on go to out2.
 __global__ __launch_bounds__(1024) void k_sum_parts(const float *__restrict__ part, int64_t parts,
-                                                    int64_t n, float *__restrict__ out) {
+                                                    int64_t n, float *__restrict__ out, int64_t n1,
+                                                    float *__restrict__ out2) {
   __shared__ float red[32][33];
   const int col = threadIdx.x & 31, turn = threadIdx.x >> 5;
   for (int64_t first = int64_t(blockIdx.x) * 32; first < n; first += int64_t(gridDim.x) * 32) {
@@ -512,23 +365,8 @@ __global__ __launch_bounds__(1024) void k_sum_parts(const float *__restrict__ pa
     // (a wavefront now has two columns: their 32 sums, added in a fixed tree)
     const float v = lanes_sum<32>(red[threadIdx.x & 31][threadIdx.x >> 5]);
     const int64_t o = first + (threadIdx.x >> 5);
-    if ((threadIdx.x & 31) == 0 && o < n) out[o] = v;
+    if ((threadIdx.x & 31) == 0 && o < n) (o < n1 ? out[o] : out2[o - n1]) = v;
   }
-}
-
-// How a row is shared: f.template run<G, NV>().
-template <typename T, typename F>
-hipError_t by_dim(int64_t dim, F f) {
-  const int64_t vecs = ceil_div<int64_t>(dim, kVec<T>);
-  if (vecs <= 8) return f.template run<8, 1>();
-  if (vecs <= 16) return f.template run<16, 1>();
-  if (vecs <= 32) return f.template run<32, 1>();
-  if (vecs <= 64) return f.template run<64, 1>();
-  if (vecs <= 128) return f.template run<64, 2>();
-  if (vecs <= 256) return f.template run<64, 4>();
-  if (vecs <= 512) return f.template run<256, 2>();
-  if (vecs <= 1024) return f.template run<256, 4>();
-  return f.template run<256, 0>();
 }
 
 template <typename T, bool E4M3>
@@ -583,10 +421,15 @@ hipError_t forward(const hg_norm_args &A, hipStream_t stream) {
 
 hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n, float *out,
                             hipStream_t stream) {
+  return launch_sum_parts(part, parts, n, out, 0, nullptr, stream);
+}
+hipError_t launch_sum_parts(const float *part, int64_t parts, int64_t n1, float *out, int64_t n2,
+                            float *out2, hipStream_t stream) {
+  const int64_t n = n1 + n2;
   if (n <= 0) return hipSuccess;
   const int64_t blocks = std::min(ceil_div<int64_t>(n, 32), kMostBlocks);
   hipLaunchKernelGGL(k_sum_parts, dim3(unsigned(blocks)), dim3(1024), 0, stream, part, parts, n,
-                     out);
+                     out, n1, out2);
   return hipGetLastError();
 }
 

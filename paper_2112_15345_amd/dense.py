@@ -26,7 +26,7 @@ import torch
 
 from . import HG_DT_BF16, HG_DT_F16, HG_DT_F32, HG_DT_NONE, _check, load_library  # noqa: F401
 
-HG_DT_E4M3 = 4
+HG_DT_E4M3, HG_DT_I8 = 4, 6
 HG_MAX_TOP = 1024
 HG_ACT_NONE, HG_ACT_RELU, HG_ACT_GELU, HG_ACT_SILU = 0, 1, 2, 3
 _ACTS = {None: HG_ACT_NONE, "none": HG_ACT_NONE, "relu": HG_ACT_RELU, "gelu": HG_ACT_GELU,
@@ -49,6 +49,22 @@ class NormGradArgs(ctypes.Structure):
                 ("weight", _P), ("dy", _P), ("dy_stride", _I64), ("dsum", _P),
                 ("dsum_stride", _I64), ("dx", _P), ("dx_stride", _I64), ("dweight", _P),
                 ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class LayerNormArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I64), ("dtype", _I32), ("out_dtype", _I32),
+                ("weight_dtype", _I32), ("bias_dtype", _I32), ("eps", _F), ("x", _P),
+                ("x_stride", _I64), ("x_rows", _I64), ("ids", _P), ("residual", _P),
+                ("residual_stride", _I64), ("weight", _P), ("bias", _P), ("y", _P),
+                ("y_stride", _I64), ("scale", _P), ("sum", _P), ("sum_stride", _I64)]
+
+
+class LayerNormGradArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I64), ("dtype", _I32), ("weight_dtype", _I32),
+                ("eps", _F), ("x", _P), ("x_stride", _I64), ("x_rows", _I64), ("ids", _P),
+                ("weight", _P), ("dy", _P), ("dy_stride", _I64), ("dsum", _P),
+                ("dsum_stride", _I64), ("dx", _P), ("dx_stride", _I64), ("dweight", _P),
+                ("dbias", _P), ("workspace", _P), ("workspace_bytes", _I64)]
 
 
 class LinearArgs(ctypes.Structure):
@@ -126,6 +142,26 @@ def rms_norm_grad(dy, x, weight=None, dsum=None, ids=None, eps: float = 1e-6,
     the gradient of sum.  dx is the gradient of x and of residual; dweight is float32 (by
     default wanted when there is a weight).  What is not wanted is None."""
     return _call("rms_norm_grad", stream, dy, x, weight, dsum, ids, eps, want_dx, want_dweight)
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, ids=None, eps: float = 1e-5,
+               out_dtype=None, stream=None):
+    """(y, sum, scale): y = (h - mean(h)) weight / sqrt(var(h) + eps) + bias per row, h = x +
+    residual (hg_layer_norm).  ids: int64 [rows], row i is x[ids[i]] (out of range: a row of NaN).
+    out_dtype: x's dtype, or torch.float8_e4m3fn or torch.int8, with scale [rows] (else None).
+    sum: h, when there is a residual (else None)."""
+    return _call("layer_norm", stream, x, weight, bias, residual, ids, eps, out_dtype)
+
+
+def layer_norm_grad(dy, x, weight=None, dsum=None, ids=None, eps: float = 1e-5,
+                    want_dx: bool = True, want_dweight: bool | None = None,
+                    want_dbias: bool = True, stream=None):
+    """(dx, dweight, dbias) of layer_norm (hg_layer_norm_grad).  x: the rows that were normalised,
+    the forward call's sum (or its x, with the same ids, when it had no residual); dsum: the
+    gradient of sum.  dx is the gradient of x and of residual; dweight (by default wanted when
+    there is a weight) and dbias are float32.  What is not wanted is None."""
+    return _call("layer_norm_grad", stream, dy, x, weight, dsum, ids, eps, want_dx, want_dweight,
+                 want_dbias)
 
 
 def linear(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=None, out_dtype=None,

@@ -1,0 +1,69 @@
+"""The C entry points of layer norms, embeddings, integers and kept rows refuse bad arguments on the
+host, before any device work, and the binding refuses unfit tensors (no GPU needed; the pointers are
+never read)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2112_15345_amd as hg
+from paper_2112_15345_amd import dense
+
+P = 0x1000  # never dereferenced
+BIG = 1 << 31
+NAN, INF = float("nan"), float("inf")
+LIB = hg.load_library()
+
+
+def layer_norm(**kw):
+    v = dict(rows=2, dim=8, dtype=1, out_dtype=1, eps=1e-6, x=P, x_stride=8, x_rows=2, y=P, y_stride=8)
+    return LIB.hg_layer_norm(ctypes.byref(dense.LayerNormArgs(**{**v, **kw})), None)
+
+
+def layer_norm_grad(**kw):
+    v = dict(rows=2, dim=8, dtype=1, eps=1e-6, x=P, x_stride=8, x_rows=2, dy=P, dy_stride=8, dx=P,
+             dx_stride=8)
+    return LIB.hg_layer_norm_grad(ctypes.byref(dense.LayerNormGradArgs(**{**v, **kw})), None)
+
+
+CASES = [
+    (layer_norm, hg.HG_EINVAL,
+     [dict(rows=-1), dict(dim=0), dict(dtype=0), dict(dtype=4), dict(dtype=6), dict(out_dtype=2),
+      dict(out_dtype=5), dict(weight_dtype=2), dict(weight_dtype=1), dict(bias_dtype=3),
+      dict(bias_dtype=1), dict(eps=-1.0), dict(eps=NAN), dict(x=None), dict(x_stride=-1),
+      dict(y=None), dict(y_stride=7), dict(sum=P, sum_stride=7), dict(out_dtype=4),
+      dict(out_dtype=6), dict(ids=P, x_rows=-1), dict(residual=P, residual_stride=-8)]),
+    (layer_norm, hg.HG_EUNSUPPORTED, [dict(rows=BIG), dict(dim=BIG)]),
+    (layer_norm_grad, hg.HG_EINVAL,
+     [dict(rows=-1), dict(dim=0), dict(dtype=6), dict(weight_dtype=3), dict(weight_dtype=1),
+      dict(dy=None), dict(x=None), dict(dx_stride=7), dict(dsum=P, dsum_stride=-1), dict(eps=INF),
+      dict(dweight=P), dict(dbias=P), dict(dbias=P, workspace=P, workspace_bytes=127)]),
+    (layer_norm_grad, hg.HG_EUNSUPPORTED, [dict(rows=BIG), dict(dim=BIG)]),
+]
+
+
+@pytest.mark.parametrize("call,status,kw", [(c, s, k) for c, s, ks in CASES for k in ks])
+def test_refused(call, status, kw):
+    assert call(**kw) == status
+    assert len(LIB.hg_last_error()) > 10
+
+
+def test_null_and_empty():
+    for f in (LIB.hg_layer_norm, LIB.hg_layer_norm_grad):
+        assert f(None, None) == hg.HG_EINVAL
+    assert layer_norm(rows=0, x=None, y=None) == hg.HG_OK
+    assert layer_norm_grad(dx=None) == hg.HG_OK
+    assert LIB.hg_layer_norm_grad_workspace(0, 8) == 0
+    assert LIB.hg_layer_norm_grad_workspace(100, 8) >= 2 * 4 * 8
+
+
+def test_tensors_that_do_not_fit():
+    x, g = torch.zeros(4, 8), torch.zeros(4, 8, requires_grad=True)
+    for call in (lambda: hg.layer_norm(g), lambda: hg.layer_norm(x, torch.zeros(8, requires_grad=True)),
+                 lambda: hg.layer_norm(x, bias=torch.zeros(8, requires_grad=True)),
+                 lambda: hg.layer_norm(x, residual=g)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    for call in (lambda: hg.layer_norm(x), lambda: hg.layer_norm_grad(g, g)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
