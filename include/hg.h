@@ -720,6 +720,46 @@ typedef struct hg_layer_norm_grad_args {
 hg_status hg_layer_norm_grad(const hg_layer_norm_grad_args *args, hipStream_t stream);
 int64_t hg_layer_norm_grad_workspace(int64_t rows, int64_t dim);
 
+/* Embedding: rows of a learned table by ID, scaled.  For i < n:
+ *   y[i] = scale table[ids[i]]
+ * in out_dtype (each a float type, whatever the table's).  An id of -1 (padding) is a row of zeros,
+ * any other outside [0, nodes) a row of NaN: nothing is read for them. */
+typedef struct hg_embed_args {
+  int64_t n, nodes, dim;      /* ids, rows of the table, its columns (dim >= 1) */
+  int32_t table_dtype, out_dtype;
+  float scale;                /* finite */
+  const void *table;          /* [nodes, dim] */
+  int64_t table_stride;
+  const int64_t *ids;         /* [n] */
+  void *y;                    /* [n, dim] */
+  int64_t y_stride;
+} hg_embed_args;
+hg_status hg_embed(const hg_embed_args *args, hipStream_t stream);
+
+/* The backward pass of hg_embed: the gradient of the table,
+ *   dtable[v] = scale sum_{i: ids[i] = v} dy[i]
+ * or, with add, dtable[v] += the same, in float32, for the rows that an id names (a gradient that
+ * is accumulated, or with scale = -rate a step of descent in place; the other rows are left as they
+ * are).  Without add every row is written, zeros where no id names it.  Ids outside [0, nodes) count
+ * for nothing.  The sums are made in a fixed order, in float32, then scaled; an id may come any
+ * number of times.  n below 2^31. */
+typedef struct hg_embed_grad_args {
+  int64_t n, nodes, dim;
+  int32_t dtype;              /* of dy */
+  int32_t out_dtype;          /* of dtable: dtype or HG_DT_F32; with add HG_DT_F32 */
+  int32_t add;                /* 0 or 1 */
+  float scale;                /* finite */
+  const void *dy;             /* [n, dim] */
+  int64_t dy_stride;
+  const int64_t *ids;         /* [n] */
+  void *dtable;               /* [nodes, dim] */
+  int64_t dtable_stride;
+  void *workspace;
+  int64_t workspace_bytes;
+} hg_embed_grad_args;
+hg_status hg_embed_grad(const hg_embed_grad_args *args, hipStream_t stream);
+int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, int32_t add);
+
 /* Matrix product with bias, activation and residual in one pass:
  *   z = x w^T + bias,  y = act(z) + residual
  * x [m, k], w [n, k] (one row per output), bias [n] or NULL, residual [m, n]

@@ -165,6 +165,53 @@ hg_status hg_layer_norm_grad(const hg_layer_norm_grad_args *a, hipStream_t strea
   return launched(launch_layer_norm_grad(*a, stream), "hg_layer_norm_grad");
 }
 
+hg_status hg_embed(const hg_embed_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_embed: NULL arguments");
+  HG_REQUIRE(a->n >= 0 && a->nodes >= 0 && a->dim >= 1, "hg_embed: n or nodes < 0, or dim < 1");
+  HG_REQUIRE(is_float(a->table_dtype), "hg_embed: table type %d", a->table_dtype);
+  HG_REQUIRE(is_float(a->out_dtype), "hg_embed: output type %d", a->out_dtype);
+  HG_REQUIRE(std::isfinite(a->scale), "hg_embed: the scale is not finite");
+  if (a->n >= kMost || a->nodes >= kMost || a->dim >= kMost)
+    return refuse(HG_EUNSUPPORTED, "hg_embed: 2^31 ids, rows or columns, or more");
+  if (a->n == 0) return HG_OK;
+  HG_REQUIRE(a->nodes == 0 || in_ok(a->table, a->table_stride),
+             "hg_embed: the table is NULL or its stride negative");
+  HG_REQUIRE(a->ids, "hg_embed: ids are NULL");
+  HG_REQUIRE(out_ok(a->y, a->y_stride, a->dim), "hg_embed: y is NULL or its stride below dim");
+  clear_pending();
+  return launched(launch_embed(*a, stream), "hg_embed");
+}
+
+int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, int32_t add) {
+  if (n <= 0 || nodes <= 0 || dim <= 0 || n >= kMost || nodes >= kMost || dim >= kMost) return 0;
+  return embed_grad_workspace(n, nodes, dim, add != 0);
+}
+
+hg_status hg_embed_grad(const hg_embed_grad_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_embed_grad: NULL arguments");
+  HG_REQUIRE(a->n >= 0 && a->nodes >= 0 && a->dim >= 1,
+             "hg_embed_grad: n or nodes < 0, or dim < 1");
+  HG_REQUIRE(is_float(a->dtype), "hg_embed_grad: type %d", a->dtype);
+  HG_REQUIRE(a->add == 0 || a->add == 1, "hg_embed_grad: add is neither 0 nor 1");
+  HG_REQUIRE(a->out_dtype == HG_DT_F32 || (!a->add && a->out_dtype == a->dtype),
+             "hg_embed_grad: output type %d", a->out_dtype);
+  HG_REQUIRE(std::isfinite(a->scale), "hg_embed_grad: the scale is not finite");
+  if (a->n >= kMost || a->nodes >= kMost || a->dim >= kMost)
+    return refuse(HG_EUNSUPPORTED, "hg_embed_grad: 2^31 ids, rows or columns, or more");
+  if (a->nodes == 0 || (a->n == 0 && a->add)) return HG_OK;
+  HG_REQUIRE(out_ok(a->dtable, a->dtable_stride, a->dim),
+             "hg_embed_grad: dtable is NULL or its stride below dim");
+  if (a->n > 0) {
+    HG_REQUIRE(in_ok(a->dy, a->dy_stride), "hg_embed_grad: dy is NULL or its stride negative");
+    HG_REQUIRE(a->ids, "hg_embed_grad: ids are NULL");
+    HG_REQUIRE(a->workspace && a->workspace_bytes >=
+                                   hg_embed_grad_workspace(a->n, a->nodes, a->dim, a->add),
+               "hg_embed_grad: workspace too small");
+  }
+  clear_pending();
+  return launched(launch_embed_grad(*a, stream), "hg_embed_grad");
+}
+
 int64_t hg_linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {
   if (m <= 0 || n <= 0 || k <= 0 || m >= kMost || n >= kMost || k >= kMost) return 0;
   return linear_workspace(m, k, n, dtype);

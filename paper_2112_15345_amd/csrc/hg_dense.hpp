@@ -30,6 +30,10 @@ int64_t rms_norm_grad_parts(int64_t rows);
 hipError_t launch_layer_norm(const hg_layer_norm_args &A, hipStream_t stream);
 hipError_t launch_layer_norm_grad(const hg_layer_norm_grad_args &A, hipStream_t stream);
 
+hipError_t launch_embed(const hg_embed_args &A, hipStream_t stream);
+hipError_t launch_embed_grad(const hg_embed_grad_args &A, hipStream_t stream);
+int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, bool add);
+
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream);
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);
 hipError_t launch_linear_grad(const hg_linear_grad_args &A, hipStream_t stream);

@@ -223,4 +223,45 @@ inline GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int3
   return g;
 }
 
+// ---- the gradient of an embedding -------------------------------------------------
+
+// Ids are sorted by least significant digits first: in one block's LDS up to kSortSmall of them,
+// past that by tiles of 256 kItems, with as few digits as 11 bits each allow.
+constexpr int64_t kSortSmall = 4096;
+constexpr int kMostDigitBits = 11;
+constexpr int kSmallDigitBits = 8;
+
+// The sorted positions are cut into chunks, whose rows are summed one after another; a run of equal
+// ids that goes past a chunk's end leaves a part in each of its chunks, which are then joined.
+struct EmbedPlan {
+  int bits, passes, digit;  // of the ids, of the sort, of a pass
+  bool small;
+  int64_t tiles, tile;
+  int64_t chunk, chunks;
+  int64_t pairs, other, counts, totals, marks, parts, total;  // byte offsets in the workspace
+};
+inline EmbedPlan embed_plan(int64_t n, int64_t nodes, int64_t dim, bool add) {
+  EmbedPlan p{};
+  while (p.bits < 32 && (nodes >> p.bits) > 0) ++p.bits;  // (ids that count for nothing are `nodes`)
+  p.small = n <= kSortSmall;
+  const int most = p.small ? kSmallDigitBits : kMostDigitBits;
+  p.passes = (p.bits + most - 1) / most;
+  p.digit = (p.bits + p.passes - 1) / p.passes;
+  p.tile = n <= int64_t(1) << 18 ? 1024 : 4096;
+  p.tiles = ceil_div<int64_t>(n, p.tile);
+  // chunks that fill the units: long ones leave fewer parts, short ones are done sooner
+  p.chunk = 8;
+  while (p.chunk < 64 && n * ceil_div<int64_t>(dim, 1024) > p.chunk * 2048) p.chunk *= 2;
+  p.chunks = ceil_div<int64_t>(n, p.chunk);
+  const int64_t bins = int64_t(1) << p.digit;
+  p.pairs = 0;
+  p.other = p.pairs + align16(n * 8);
+  p.counts = p.other + (p.small ? 0 : align16(n * 8));
+  p.totals = p.counts + (p.small ? 0 : align16(bins * p.tiles * 4));
+  p.marks = p.totals + (p.small ? 0 : align16(bins * 4));
+  p.parts = p.marks + (add ? 0 : align16(nodes));
+  p.total = p.parts + 2 * p.chunks * dim * 4;
+  return p;
+}
+
 }  // namespace hg

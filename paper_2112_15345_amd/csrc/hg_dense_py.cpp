@@ -11,6 +11,7 @@
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -38,6 +39,9 @@ struct Api {
   decltype(&hg_layer_norm) layer_norm = nullptr;
   decltype(&hg_layer_norm_grad) layer_norm_grad = nullptr;
   decltype(&hg_layer_norm_grad_workspace) layer_norm_grad_workspace = nullptr;
+  decltype(&hg_embed) embed = nullptr;
+  decltype(&hg_embed_grad) embed_grad = nullptr;
+  decltype(&hg_embed_grad_workspace) embed_grad_workspace = nullptr;
 } api;
 constexpr int kEntries = int(sizeof(Api) / sizeof(void *));
 
@@ -90,6 +94,10 @@ void check_type(const at::Tensor &t, const char *name, Types types) {
   for (at::ScalarType s : types)
     if (t.scalar_type() == s) return;
   throw Unfit(std::string(name) + ": unsupported dtype " + at::toString(t.scalar_type()));
+}
+void check_float(at::ScalarType t, const char *name) {
+  if (t != at::kFloat && t != at::kHalf && t != at::kBFloat16)
+    throw Unfit(std::string(name) + ": unsupported dtype " + at::toString(t));
 }
 void check_device(const at::Tensor &t, const char *name, std::optional<at::Device> device) {
   if (!t.device().is_cuda() || (device && t.device() != *device))
@@ -405,6 +413,86 @@ PyObject *layer_norm_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
+// embed(table, ids, scale, out_dtype) -> (y,)
+PyObject *embed(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(n, 4, [&]() -> PyObject * {
+    no_gradient({args[0]});
+    const at::Tensor table = matrix(args[0], "table", kFloats);
+    const auto dev = table.device();
+    const at::Tensor ids = vector(args[1], "ids", {at::kLong}, dev, -1);
+    const auto out = type_or(args[3], table.scalar_type(), "out_dtype");
+    check_float(out, "out_dtype");
+    const int64_t rows = ids.size(0), dim = table.size(1);
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor y = make({rows, dim}, out, dev);
+    hg_embed_args a{};
+    a.n = rows;
+    a.nodes = table.size(0);
+    a.dim = dim;
+    a.table_dtype = code_of(table.scalar_type());
+    a.out_dtype = code_of(out);
+    a.scale = float(number(args[2]));
+    a.table = ptr(table);
+    a.table_stride = stride(table);
+    a.ids = static_cast<const int64_t *>(ptr(ids));
+    a.y = ptr(y);
+    a.y_stride = dim;
+    return result(api.embed(&a, current_stream(dev)), {y});
+  });
+}
+
+// embed_grad(dy, ids, nodes, scale, out_dtype, into) -> (dtable,)
+PyObject *embed_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject * {
+    no_gradient({args[5]});  // (written in place)
+    const at::Tensor dy = matrix(args[0], "dy", kFloats);
+    const auto dev = dy.device();
+    const auto type = dy.scalar_type();
+    const int64_t rows = dy.size(0), dim = dy.size(1);
+    const at::Tensor ids = vector(args[1], "ids", {at::kLong}, dev, rows);
+    const int64_t nodes = integer(args[2]);
+    const bool add = args[5] != Py_None;
+    const auto out = type_or(args[4], at::kFloat, "out_dtype");
+    if (out != at::kFloat && (add || out != type))
+      throw Unfit(add ? "out_dtype: into is float32" : "out_dtype: neither dy's nor float32");
+    if (nodes < 0) throw Unfit("nodes: negative");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor d;
+    if (add) {
+      const at::Tensor *const t = given(args[5], "into");
+      matrix(args[5], "into", {at::kFloat}, dev, nodes, dim);
+      if ((dim > 1 && t->stride(1) != 1) || (nodes > 1 && t->stride(0) < dim))
+        throw Unfit("into: its columns are not contiguous, or its rows overlap");
+      if (t->is_inference() && !c10::InferenceMode::is_enabled())
+        throw Unfit("into: an inference tensor is not written outside of inference mode");
+      d = *t;
+    } else {
+      d = make({nodes, dim}, out, dev);
+    }
+    const at::Tensor ws =
+        workspace(api.embed_grad_workspace(rows, nodes, dim, add), dev);
+    hg_embed_grad_args a{};
+    a.n = rows;
+    a.nodes = nodes;
+    a.dim = dim;
+    a.dtype = code_of(type);
+    a.out_dtype = code_of(out);
+    a.add = add;
+    a.scale = float(number(args[3]));
+    a.dy = ptr(dy);
+    a.dy_stride = stride(dy);
+    a.ids = static_cast<const int64_t *>(ptr(ids));
+    a.dtable = ptr(d);
+    a.dtable_stride = stride(d);
+    a.workspace = ptr(ws);
+    a.workspace_bytes = bytes_of(ws);
+    const hg_status st = api.embed_grad(&a, current_stream(dev));
+    // (what autograd has kept of it elsewhere is no longer its value)
+    if (add && st == HG_OK && !d.is_inference()) d.unsafeGetTensorImpl()->bump_version();
+    return result(st, {d});
+  });
+}
+
 // linear(x, w, bias, act, residual, x_scale, w_scale, out_dtype, keep_pre) -> (y, pre)
 PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> PyObject * {
@@ -584,6 +672,8 @@ PyMethodDef methods[] = {method<bind>("bind"),
                          method<rms_norm_grad>("rms_norm_grad"),
                          method<layer_norm>("layer_norm"),
                          method<layer_norm_grad>("layer_norm_grad"),
+                         method<embed>("embed"),
+                         method<embed_grad>("embed_grad"),
                          method<linear>("linear"),
                          method<linear_grad>("linear_grad"),
                          method<distill>("distill"),

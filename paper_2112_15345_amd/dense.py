@@ -67,6 +67,19 @@ class LayerNormGradArgs(ctypes.Structure):
                 ("dbias", _P), ("workspace", _P), ("workspace_bytes", _I64)]
 
 
+class EmbedArgs(ctypes.Structure):
+    _fields_ = [("n", _I64), ("nodes", _I64), ("dim", _I64), ("table_dtype", _I32),
+                ("out_dtype", _I32), ("scale", _F), ("table", _P), ("table_stride", _I64),
+                ("ids", _P), ("y", _P), ("y_stride", _I64)]
+
+
+class EmbedGradArgs(ctypes.Structure):
+    _fields_ = [("n", _I64), ("nodes", _I64), ("dim", _I64), ("dtype", _I32), ("out_dtype", _I32),
+                ("add", _I32), ("scale", _F), ("dy", _P), ("dy_stride", _I64), ("ids", _P),
+                ("dtable", _P), ("dtable_stride", _I64), ("workspace", _P),
+                ("workspace_bytes", _I64)]
+
+
 class LinearArgs(ctypes.Structure):
     _fields_ = [("m", _I64), ("k", _I64), ("n", _I64), ("dtype", _I32), ("out_dtype", _I32),
                 ("bias_dtype", _I32), ("act", _I32), ("x", _P), ("x_stride", _I64),
@@ -162,6 +175,21 @@ def layer_norm_grad(dy, x, weight=None, dsum=None, ids=None, eps: float = 1e-5,
     there is a weight) and dbias are float32.  What is not wanted is None."""
     return _call("layer_norm_grad", stream, dy, x, weight, dsum, ids, eps, want_dx, want_dweight,
                  want_dbias)
+
+
+def embed(table, ids, scale: float = 1.0, out_dtype=None, stream=None):
+    """scale table[ids] (hg_embed), in out_dtype (default: the table's).  ids: int64 [n]; -1
+    (padding) is a row of zeros, any other out of range a row of NaN."""
+    return _call("embed", stream, table, ids, scale, out_dtype)[0]
+
+
+def embed_grad(dy, ids, nodes: int, scale: float = 1.0, out_dtype=None, into=None, stream=None):
+    """The gradient of embed's table [nodes, dim] (hg_embed_grad), summed in a fixed order:
+    scale times the sum of dy's rows over the positions of each id, in out_dtype (float32 by
+    default, or dy's).  Ids out of range count for nothing.  into: a float32 table that it is
+    added to in place, and that is returned; rows that no id names are not touched (with scale
+    = -rate a step of descent)."""
+    return _call("embed_grad", stream, dy, ids, nodes, scale, out_dtype, into)[0]
 
 
 def linear(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=None, out_dtype=None,

@@ -26,6 +26,18 @@ def layer_norm_grad(**kw):
     return LIB.hg_layer_norm_grad(ctypes.byref(dense.LayerNormGradArgs(**{**v, **kw})), None)
 
 
+def embed(**kw):
+    v = dict(n=2, nodes=5, dim=8, table_dtype=1, out_dtype=3, scale=1.0, table=P, table_stride=8, ids=P,
+             y=P, y_stride=8)
+    return LIB.hg_embed(ctypes.byref(dense.EmbedArgs(**{**v, **kw})), None)
+
+
+def embed_grad(**kw):
+    v = dict(n=2, nodes=5, dim=8, dtype=3, out_dtype=1, scale=1.0, dy=P, dy_stride=8, ids=P, dtable=P,
+             dtable_stride=8, workspace=P, workspace_bytes=1 << 40)
+    return LIB.hg_embed_grad(ctypes.byref(dense.EmbedGradArgs(**{**v, **kw})), None)
+
+
 CASES = [
     (layer_norm, hg.HG_EINVAL,
      [dict(rows=-1), dict(dim=0), dict(dtype=0), dict(dtype=4), dict(dtype=6), dict(out_dtype=2),
@@ -39,6 +51,17 @@ CASES = [
       dict(dy=None), dict(x=None), dict(dx_stride=7), dict(dsum=P, dsum_stride=-1), dict(eps=INF),
       dict(dweight=P), dict(dbias=P), dict(dbias=P, workspace=P, workspace_bytes=127)]),
     (layer_norm_grad, hg.HG_EUNSUPPORTED, [dict(rows=BIG), dict(dim=BIG)]),
+    (embed, hg.HG_EINVAL,
+     [dict(n=-1), dict(nodes=-1), dict(dim=0), dict(table_dtype=0), dict(table_dtype=4),
+      dict(out_dtype=6), dict(scale=NAN), dict(scale=INF), dict(table=None), dict(table_stride=-1),
+      dict(ids=None), dict(y=None), dict(y_stride=7)]),
+    (embed, hg.HG_EUNSUPPORTED, [dict(n=BIG), dict(nodes=BIG), dict(dim=BIG)]),
+    (embed_grad, hg.HG_EINVAL,
+     [dict(n=-1), dict(nodes=-1), dict(dim=0), dict(dtype=0), dict(dtype=4), dict(out_dtype=2),
+      dict(add=2), dict(add=-1), dict(add=1, out_dtype=3), dict(scale=-INF), dict(dy=None),
+      dict(dy_stride=-1), dict(ids=None), dict(dtable=None), dict(dtable_stride=7),
+      dict(workspace=None), dict(workspace_bytes=15)]),
+    (embed_grad, hg.HG_EUNSUPPORTED, [dict(n=BIG), dict(nodes=BIG), dict(dim=BIG)]),
 ]
 
 
@@ -49,11 +72,20 @@ def test_refused(call, status, kw):
 
 
 def test_null_and_empty():
-    for f in (LIB.hg_layer_norm, LIB.hg_layer_norm_grad):
+    for f in (LIB.hg_layer_norm, LIB.hg_layer_norm_grad, LIB.hg_embed, LIB.hg_embed_grad):
         assert f(None, None) == hg.HG_EINVAL
     assert layer_norm(rows=0, x=None, y=None) == hg.HG_OK
     assert layer_norm_grad(dx=None) == hg.HG_OK
+    assert embed(n=0, table=None, ids=None, y=None) == hg.HG_OK
+    assert embed_grad(n=0, add=1, dtable=None) == hg.HG_OK
+    assert embed_grad(nodes=0, dtable=None) == hg.HG_OK
     assert LIB.hg_layer_norm_grad_workspace(0, 8) == 0
+    assert LIB.hg_embed_grad_workspace(0, 9, 8, 0) == 0
+    for n in (1, 4096, 4097, 1 << 18, (1 << 31) - 1):
+        for nodes in (1, 1000, (1 << 31) - 1):
+            w = [LIB.hg_embed_grad_workspace(n, nodes, 24, add) for add in (0, 1)]
+            # the pairs and, without add, a byte for each row
+            assert w[1] >= 8 * n and w[0] - w[1] >= nodes
     assert LIB.hg_layer_norm_grad_workspace(100, 8) >= 2 * 4 * 8
 
 
@@ -61,9 +93,12 @@ def test_tensors_that_do_not_fit():
     x, g = torch.zeros(4, 8), torch.zeros(4, 8, requires_grad=True)
     for call in (lambda: hg.layer_norm(g), lambda: hg.layer_norm(x, torch.zeros(8, requires_grad=True)),
                  lambda: hg.layer_norm(x, bias=torch.zeros(8, requires_grad=True)),
-                 lambda: hg.layer_norm(x, residual=g)):
+                 lambda: hg.layer_norm(x, residual=g), lambda: hg.embed(g, torch.zeros(2).long()),
+                 lambda: hg.embed_grad(x, torch.zeros(4).long(), 4, into=g)):
         with pytest.raises(ValueError, match="gradient"):
             call()
-    for call in (lambda: hg.layer_norm(x), lambda: hg.layer_norm_grad(g, g)):
+    for call in (lambda: hg.layer_norm(x), lambda: hg.layer_norm_grad(g, g),
+                 lambda: hg.embed(x, torch.zeros(2).long()),
+                 lambda: hg.embed_grad(g, torch.zeros(4).long(), 4)):
         with pytest.raises(ValueError, match="GPU"):
             call()
