@@ -760,20 +760,54 @@ typedef struct hg_embed_grad_args {
 hg_status hg_embed_grad(const hg_embed_grad_args *args, hipStream_t stream);
 int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, int32_t add);
 
+/* Rows in 8-bit integers, for products of integers or to keep activations in half the memory or
+ * less until the backward pass.  Over each row (group 0), or over each HG_KEPT_GROUP columns of a row
+ * (group HG_KEPT_GROUP; the last group may be shorter):
+ *   scale = max(max_j |x_j| / 127, 2^-126),  q_j = x_j / scale
+ * in float32, rounded to the nearest integer (of two as near, the even one), so that q_j scale
+ * stands for x_j, within half a scale of it.  A row (or group) with a NaN or an infinity is zeros with a
+ * scale of NaN. */
+#define HG_KEPT_GROUP 128
+typedef struct hg_quantize_args {
+  int64_t rows, dim;          /* dim >= 1 */
+  int32_t dtype, group;       /* group: 0 or HG_KEPT_GROUP */
+  const void *x;
+  int64_t x_stride;
+  int8_t *q;                  /* [rows, dim] */
+  int64_t q_stride;
+  float *scale;               /* [rows], or [rows, ceil(dim / group)], contiguous */
+} hg_quantize_args;
+hg_status hg_quantize(const hg_quantize_args *args, hipStream_t stream);
+
+/* What such rows stand for: x_j = q_j scale, rounded once to `dtype`. */
+typedef struct hg_dequantize_args {
+  int64_t rows, dim;
+  int32_t dtype, group;
+  const int8_t *q;
+  int64_t q_stride;
+  const float *scale;
+  void *x;
+  int64_t x_stride;
+} hg_dequantize_args;
+hg_status hg_dequantize(const hg_dequantize_args *args, hipStream_t stream);
+
 /* Matrix product with bias, activation and residual in one pass:
  *   z = x w^T + bias,  y = act(z) + residual
  * x [m, k], w [n, k] (one row per output), bias [n] or NULL, residual [m, n]
  * or NULL, y [m, n]; pre (NULL: not written) receives z for the backward pass.
  * k may be 0 (the product is then 0).
  * dtype of x and w: float32, float16, bfloat16, with y, pre and residual in the
- * same type; or HG_DT_E4M3 with a scale per row of x and of w,
+ * same type; or HG_DT_E4M3 or HG_DT_I8 with a scale per row of x and of w,
  *   z_ij = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,
  * and y, pre and residual in out_dtype (float32, float16 or bfloat16).
+ * HG_DT_I8 is the same with 8-bit integers (-128 .. 127), whose sum over k is exact (k up to 131071,
+ * HG_EUNSUPPORTED past it; rounded to float32 once, or once in each part of a product whose k is
+ * cut).
  * float32 products are made of 16-bit pieces that add up to the elements (of
  * elements below 2^-108 in size the pieces may lose the lower bits), and are
  * as exact as products in 32 bits; results that are not finite that way, as
  * where terms pass the largest float32, are made by products in 32 bits.
- * 8-bit elements are multiplied as bfloat16.
+ * e4m3 elements are multiplied as bfloat16.
  * act: gelu is z / (1 + exp(-2 u)), u = sqrt(2/pi) (z + 0.044715 z^3) (its tanh
  * form); silu is z / (1 + exp(-z)).
  * y may be residual with the same stride. */
@@ -788,10 +822,10 @@ typedef struct hg_linear_args {
   int32_t act;                /* HG_ACT_* */
   const void *x;
   int64_t x_stride;
-  const float *x_scale;       /* [m], with HG_DT_E4M3 */
+  const float *x_scale;       /* [m], with HG_DT_E4M3 and HG_DT_I8 */
   const void *w;
   int64_t w_stride;
-  const float *w_scale;       /* [n], with HG_DT_E4M3 */
+  const float *w_scale;       /* [n], with HG_DT_E4M3 and HG_DT_I8 */
   const void *bias;
   const void *residual;
   int64_t residual_stride;
@@ -833,6 +867,21 @@ typedef struct hg_linear_grad_args {
 } hg_linear_grad_args;
 hg_status hg_linear_grad(const hg_linear_grad_args *args, hipStream_t stream);
 int64_t hg_linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act);
+
+/* The backward pass of hg_linear from activations that were kept in 8-bit integers (hg_quantize):
+ * x where x_scale is given, pre where pre_scale is, each with `group` as it was kept; the other
+ * one (or pre with HG_ACT_NONE) as in hg_linear_grad.  Results and roundings are those of
+ * hg_linear_grad on the values that the integers stand for (a pre that was rounded to 0 is 0: relu's
+ * slope there is 0); x's are rounded to `dtype` once. */
+typedef struct hg_linear_grad_kept_args {
+  hg_linear_grad_args grad;   /* x and pre: int8 with strides in elements, where they are kept; the
+                                 workspace's size from hg_linear_grad_kept_workspace */
+  int32_t group;              /* 0 or HG_KEPT_GROUP */
+  const float *x_scale;       /* [m] or [m, ceil(k / group)], or NULL: x is in dtype */
+  const float *pre_scale;     /* [m] or [m, ceil(n / group)], or NULL: pre is in dtype */
+} hg_linear_grad_kept_args;
+hg_status hg_linear_grad_kept(const hg_linear_grad_kept_args *args, hipStream_t stream);
+int64_t hg_linear_grad_kept_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act);
 
 /* Distillation from a teacher's top logits.  Row i lists up to `top` classes
  * with the teacher's logits; an entry with id -1 or a teacher logit of -inf is

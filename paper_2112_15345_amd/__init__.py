@@ -17,7 +17,7 @@ is not built; there is no CPU path.
     x = g.gather_features(b, ntype)
 
 The dense operators that a model runs on such rows (rms_norm, layer_norm, linear, distill and
-their backward passes), and embed for rows that it learns, are in `dense`, and under this package's name.
+their backward passes), embed for rows that it learns, and quantize for rows that it keeps, are in `dense`, and under this package's name.
 """
 from __future__ import annotations
 
@@ -60,7 +60,8 @@ ABI_SYMBOLS = ("hg_create", "hg_destroy", "hg_retire_stream", "hg_sample_blocks"
                "hg_rms_norm", "hg_rms_norm_grad", "hg_rms_norm_grad_workspace",
                "hg_linear", "hg_linear_workspace", "hg_linear_grad", "hg_linear_grad_workspace",
                "hg_distill", "hg_layer_norm", "hg_layer_norm_grad", "hg_layer_norm_grad_workspace",
-               "hg_embed", "hg_embed_grad", "hg_embed_grad_workspace")
+               "hg_embed", "hg_embed_grad", "hg_embed_grad_workspace", "hg_quantize",
+               "hg_dequantize", "hg_linear_grad_kept", "hg_linear_grad_kept_workspace")
 
 HG_MAX_NEG = 64
 HG_MAX_TIMED_HOPS = 8
@@ -172,6 +173,10 @@ def _bind(lib: ctypes.CDLL) -> ctypes.CDLL:
         "hg_embed": ([_P, _P], _I32),
         "hg_embed_grad": ([_P, _P], _I32),
         "hg_embed_grad_workspace": ([_I64, _I64, _I64, _I32], _I64),
+        "hg_quantize": ([_P, _P], _I32),
+        "hg_dequantize": ([_P, _P], _I32),
+        "hg_linear_grad_kept": ([_P, _P], _I32),
+        "hg_linear_grad_kept_workspace": ([_I64, _I64, _I64, _I32, _I32], _I64),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -218,7 +223,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             lib.hg_linear_workspace, lib.hg_linear_grad, lib.hg_linear_grad_workspace,
             lib.hg_distill, lib.hg_layer_norm, lib.hg_layer_norm_grad,
             lib.hg_layer_norm_grad_workspace, lib.hg_embed, lib.hg_embed_grad,
-            lib.hg_embed_grad_workspace)))
+            lib.hg_embed_grad_workspace, lib.hg_quantize, lib.hg_dequantize,
+            lib.hg_linear_grad_kept, lib.hg_linear_grad_kept_workspace)))
         _views, _dense = views, dense
         _lib = lib
     return _lib
@@ -962,5 +968,6 @@ def bench_philox(rng_seed: int, hop: int, etype: int, n_groups: int, lim: int,
 
 
 from .dense import (HG_ACT_GELU, HG_ACT_NONE, HG_ACT_RELU, HG_ACT_SILU,  # noqa: E402,F401
-                    HG_DT_E4M3, HG_DT_I8, HG_MAX_TOP, distill, embed, embed_grad,
-                    layer_norm, layer_norm_grad, linear, linear_grad, rms_norm, rms_norm_grad)
+                    HG_DT_E4M3, HG_DT_I8, HG_KEPT_GROUP, HG_MAX_TOP, dequantize, distill,
+                    embed, embed_grad, layer_norm, layer_norm_grad, linear, linear_grad, quantize,
+                    rms_norm, rms_norm_grad)

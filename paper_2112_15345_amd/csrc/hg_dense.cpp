@@ -20,6 +20,8 @@ hg_status refuse(hg_status st, const char *fmt, ...) {
 }
 
 constexpr int64_t kMost = int64_t(1) << 31;
+// Products of integers of up to 2^14 each, whose sum is below 2^31.
+constexpr int64_t kMostIntegers = (int64_t(1) << 17) - 1;
 
 bool is_float(int32_t dt) { return dt == HG_DT_F32 || dt == HG_DT_F16 || dt == HG_DT_BF16; }
 
@@ -27,6 +29,16 @@ bool is_8_bits(int32_t dt) { return dt == HG_DT_E4M3 || dt == HG_DT_I8; }
 // The type of a weight or bias over columns of `dtype`.
 bool columns_ok(int32_t dt, int32_t dtype) {
   return dt == HG_DT_NONE || dt == HG_DT_F32 || dt == dtype;
+}
+
+bool group_ok(int32_t group) { return group == 0 || group == HG_KEPT_GROUP; }
+Kept kept(const void *q, int64_t stride, const float *scale, int32_t group, int64_t cols) {
+  Kept k;
+  k.p = q;
+  k.stride = stride;
+  k.scale = scale;
+  k.groups = group ? ceil_div<int64_t>(cols, group) : 1;
+  return k;
 }
 
 #define HG_REQUIRE(cond, ...) \
@@ -212,6 +224,39 @@ hg_status hg_embed_grad(const hg_embed_grad_args *a, hipStream_t stream) {
   return launched(launch_embed_grad(*a, stream), "hg_embed_grad");
 }
 
+hg_status hg_quantize(const hg_quantize_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_quantize: NULL arguments");
+  HG_REQUIRE(a->rows >= 0 && a->dim >= 1, "hg_quantize: rows < 0 or dim < 1");
+  HG_REQUIRE(is_float(a->dtype), "hg_quantize: type %d", a->dtype);
+  HG_REQUIRE(group_ok(a->group), "hg_quantize: group %d", a->group);
+  if (a->rows >= kMost || a->dim >= kMost)
+    return refuse(HG_EUNSUPPORTED, "hg_quantize: 2^31 rows or columns, or more");
+  if (a->rows == 0) return HG_OK;
+  HG_REQUIRE(in_ok(a->x, a->x_stride), "hg_quantize: x is NULL or its stride negative");
+  HG_REQUIRE(out_ok(a->q, a->q_stride, a->dim), "hg_quantize: q is NULL or its stride below dim");
+  HG_REQUIRE(a->scale, "hg_quantize: scale is NULL");
+  clear_pending();
+  return launched(launch_quantize(*a, stream), "hg_quantize");
+}
+
+hg_status hg_dequantize(const hg_dequantize_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_dequantize: NULL arguments");
+  HG_REQUIRE(a->rows >= 0 && a->dim >= 1, "hg_dequantize: rows < 0 or dim < 1");
+  HG_REQUIRE(is_float(a->dtype), "hg_dequantize: type %d", a->dtype);
+  HG_REQUIRE(group_ok(a->group), "hg_dequantize: group %d", a->group);
+  if (a->rows >= kMost || a->dim >= kMost)
+    return refuse(HG_EUNSUPPORTED, "hg_dequantize: 2^31 rows or columns, or more");
+  if (a->rows == 0) return HG_OK;
+  HG_REQUIRE(in_ok(a->q, a->q_stride), "hg_dequantize: q is NULL or its stride negative");
+  HG_REQUIRE(a->scale, "hg_dequantize: scale is NULL");
+  HG_REQUIRE(out_ok(a->x, a->x_stride, a->dim),
+             "hg_dequantize: x is NULL or its stride below dim");
+  clear_pending();
+  return launched(launch_dequantize(kept(a->q, a->q_stride, a->scale, a->group, a->dim), a->rows,
+                                    a->dim, a->dim, a->dtype, a->x, a->x_stride, stream),
+                  "hg_dequantize");
+}
+
 int64_t hg_linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {
   if (m <= 0 || n <= 0 || k <= 0 || m >= kMost || n >= kMost || k >= kMost) return 0;
   return linear_workspace(m, k, n, dtype);
@@ -220,17 +265,20 @@ int64_t hg_linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype) {
 hg_status hg_linear(const hg_linear_args *a, hipStream_t stream) {
   HG_REQUIRE(a, "hg_linear: NULL arguments");
   HG_REQUIRE(a->m >= 0 && a->k >= 0 && a->n >= 0, "hg_linear: a negative size");
-  HG_REQUIRE(is_float(a->dtype) || a->dtype == HG_DT_E4M3, "hg_linear: type %d", a->dtype);
-  HG_REQUIRE(a->dtype == HG_DT_E4M3 ? is_float(a->out_dtype) : a->out_dtype == a->dtype,
+  HG_REQUIRE(is_float(a->dtype) || is_8_bits(a->dtype), "hg_linear: type %d", a->dtype);
+  HG_REQUIRE(is_8_bits(a->dtype) ? is_float(a->out_dtype) : a->out_dtype == a->dtype,
              "hg_linear: output type %d with type %d", a->out_dtype, a->dtype);
   HG_REQUIRE(!a->bias || is_float(a->bias_dtype), "hg_linear: bias type %d", a->bias_dtype);
   HG_REQUIRE(a->act >= HG_ACT_NONE && a->act <= HG_ACT_SILU, "hg_linear: activation %d", a->act);
   if (a->m >= kMost || a->k >= kMost || a->n >= kMost)
     return refuse(HG_EUNSUPPORTED, "hg_linear: a size of 2^31 or more");
+  if (a->dtype == HG_DT_I8 && a->k > kMostIntegers)
+    return refuse(HG_EUNSUPPORTED, "hg_linear: more than %d products of integers in a sum",
+                  int(kMostIntegers));
   if (a->m == 0 || a->n == 0) return HG_OK;
   HG_REQUIRE(a->k == 0 || (in_ok(a->x, a->x_stride) && in_ok(a->w, a->w_stride)),
              "hg_linear: x or w is NULL or its stride negative");
-  HG_REQUIRE(a->dtype != HG_DT_E4M3 || (a->x_scale && a->w_scale), "hg_linear: 8 bits need scales");
+  HG_REQUIRE(!is_8_bits(a->dtype) || (a->x_scale && a->w_scale), "hg_linear: 8 bits need scales");
   HG_REQUIRE(!a->residual || a->residual_stride >= 0, "hg_linear: residual stride");
   HG_REQUIRE(out_ok(a->y, a->y_stride, a->n), "hg_linear: y is NULL or its stride below n");
   HG_REQUIRE(!a->pre || a->pre_stride >= a->n, "hg_linear: pre's stride below n");
@@ -243,11 +291,11 @@ hg_status hg_linear(const hg_linear_args *a, hipStream_t stream) {
 
 int64_t hg_linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
   if (m <= 0 || n <= 0 || k < 0 || m >= kMost || n >= kMost || k >= kMost) return 0;
-  return linear_grad_workspace(m, k, n, dtype, act);
+  return linear_grad_workspace(m, k, n, dtype, act, false);
 }
 
-hg_status hg_linear_grad(const hg_linear_grad_args *a, hipStream_t stream) {
-  HG_REQUIRE(a, "hg_linear_grad: NULL arguments");
+static hg_status linear_grad(const hg_linear_grad_args *a, const Kept &x, const Kept &pre,
+                             int64_t need, hipStream_t stream) {
   HG_REQUIRE(a->m >= 0 && a->k >= 0 && a->n >= 0, "hg_linear_grad: a negative size");
   HG_REQUIRE(is_float(a->dtype), "hg_linear_grad: type %d", a->dtype);
   HG_REQUIRE(!a->dw || a->dw_dtype == a->dtype || a->dw_dtype == HG_DT_F32,
@@ -266,13 +314,35 @@ hg_status hg_linear_grad(const hg_linear_grad_args *a, hipStream_t stream) {
                "hg_linear_grad: w is NULL or its stride negative");
     HG_REQUIRE(a->k == 0 || !a->dw || in_ok(a->x, a->x_stride),
                "hg_linear_grad: x is NULL or its stride negative");
-    const int64_t need = hg_linear_grad_workspace(a->m, a->k, a->n, a->dtype, a->act);
     HG_REQUIRE(need == 0 || (a->workspace && a->workspace_bytes >= need),
                "hg_linear_grad: workspace too small");
   }
   clear_pending();
-  return launched(launch_linear_grad(*a, stream), "hg_linear_grad");
+  return launched(launch_linear_grad(*a, x, pre, stream), "hg_linear_grad");
 }
+
+hg_status hg_linear_grad(const hg_linear_grad_args *a, hipStream_t stream) {
+  HG_REQUIRE(a, "hg_linear_grad: NULL arguments");
+  return linear_grad(a, Kept(), Kept(),
+                     hg_linear_grad_workspace(a->m, a->k, a->n, a->dtype, a->act), stream);
+}
+
+int64_t hg_linear_grad_kept_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
+  if (m <= 0 || n <= 0 || k < 0 || m >= kMost || n >= kMost || k >= kMost) return 0;
+  return linear_grad_workspace(m, k, n, dtype, act, true);
+}
+
+hg_status hg_linear_grad_kept(const hg_linear_grad_kept_args *args, hipStream_t stream) {
+  HG_REQUIRE(args, "hg_linear_grad_kept: NULL arguments");
+  HG_REQUIRE(group_ok(args->group), "hg_linear_grad_kept: group %d", args->group);
+  const hg_linear_grad_args &a = args->grad;
+  Kept x, pre;
+  if (args->x_scale) x = kept(a.x, a.x_stride, args->x_scale, args->group, a.k);
+  if (args->pre_scale) pre = kept(a.pre, a.pre_stride, args->pre_scale, args->group, a.n);
+  return linear_grad(&a, x, pre, hg_linear_grad_kept_workspace(a.m, a.k, a.n, a.dtype, a.act),
+                     stream);
+}
+
 
 hg_status hg_distill(const hg_distill_args *a, hipStream_t stream) {
   HG_REQUIRE(a, "hg_distill: NULL arguments");

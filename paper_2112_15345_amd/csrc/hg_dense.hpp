@@ -34,10 +34,19 @@ hipError_t launch_embed(const hg_embed_args &A, hipStream_t stream);
 hipError_t launch_embed_grad(const hg_embed_grad_args &A, hipStream_t stream);
 int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, bool add);
 
+struct Kept;
+hipError_t launch_quantize(const hg_quantize_args &A, hipStream_t stream);
+// Rows of `cols` values, and zeros from there to out_cols.
+hipError_t launch_dequantize(const Kept &K, int64_t rows, int64_t cols, int64_t out_cols,
+                             int32_t dtype, void *out, int64_t stride, hipStream_t stream);
+
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream);
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);
-hipError_t launch_linear_grad(const hg_linear_grad_args &A, hipStream_t stream);
-int64_t linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act);
+// x and pre: rows that were kept in 8 bits (p not NULL), in the place of A's.
+hipError_t launch_linear_grad(const hg_linear_grad_args &A, const Kept &x, const Kept &pre,
+                              hipStream_t stream);
+int64_t linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act,
+                              bool kept_x);
 
 hipError_t launch_distill(const hg_distill_args &A, hipStream_t stream);
 
@@ -180,5 +189,31 @@ __device__ __forceinline__ uint32_t lanes_max_bits(uint32_t v) {
     return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
   }));
 }
+
+// Rows in 8-bit integers, a scale for each (groups 1), or for each HG_KEPT_GROUP of its columns.
+struct Kept {
+  const void *p = nullptr;
+  int64_t stride = 0;
+  const float *scale = nullptr;  // [rows, groups]
+  int64_t groups = 1;
+  __device__ __forceinline__ float scale_of(int64_t row, int64_t c) const {
+    return scale[groups == 1 ? row : row * groups + c / HG_KEPT_GROUP];
+  }
+  // N values from column c (a multiple of N) on, n of them in the row.
+  template <int N>
+  __device__ __forceinline__ void load(int64_t row, int64_t c, int n, float *v) const {
+    static_assert(HG_KEPT_GROUP % N == 0, "one scale for all");
+    if (n <= 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = 0.0f;
+      return;
+    }
+    Vec<int8_t, N> q;
+    q.load(static_cast<const int8_t *>(p) + row * stride + c, n);
+    const float s = scale_of(row, c);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = k < n ? float(q.e[k]) * s : 0.0f;
+  }
+};
 
 }  // namespace hg

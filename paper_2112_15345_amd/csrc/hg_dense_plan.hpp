@@ -16,10 +16,12 @@ constexpr T ceil_div(T a, T b) {
 
 inline int64_t align16(int64_t b) { return (b + 15) / 16 * 16; }
 inline int64_t size_of(int32_t dtype) {
-  return dtype == HG_DT_F32 ? 4 : (dtype == HG_DT_E4M3 ? 1 : 2);
+  return dtype == HG_DT_F32 ? 4 : (dtype == HG_DT_E4M3 || dtype == HG_DT_I8 ? 1 : 2);
 }
 // Elements of q in 128 bytes of what the matrix instructions take.
-inline int64_t slab_of(int32_t dtype) { return dtype == HG_DT_F32 ? 32 : 64; }
+inline int64_t slab_of(int32_t dtype) {
+  return dtype == HG_DT_F32 ? 32 : (dtype == HG_DT_I8 ? 128 : 64);
+}
 
 // How a product is cut: its tiles, how many slabs are in LDS, and the parts of its depth.
 // A compute unit that multiplies one tile waits for its loads unless several slabs are in
@@ -69,9 +71,9 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t depth, int64_t slab, boo
   if (rows > 0 && cols > 0) {
     const int64_t large = tiles_of(rows, cols, 256, 256), tall = tiles_of(rows, cols, 256, 128);
     const int64_t medium = tiles_of(rows, cols, 128, 128);
-    if (both && tall >= kUnits && slab == 64)
+    if (both && tall >= kUnits && slab != 32)
       p = Plan{Cut::kTall, 256, 128, 1, 0, rows};
-    else if (!both && large >= 2 * kUnits && depth >= 8 * slab && slab == 64)
+    else if (!both && large >= 2 * kUnits && depth >= 8 * slab && slab != 32)
       p = Plan{Cut::kLarge, 256, 256, 1, 0, rows};
     else if (medium <= kUnits / 2 && medium * (depth / (32 * slab)) <= kUnits / 2)
       p = Plan{Cut::kSmall, 64, 64, 1, 0, rows};
@@ -203,20 +205,23 @@ struct GradSpace {  // byte offsets in the workspace
   int64_t dz_stride;  // of dz in the workspace
   bool dz_laid, laid;
 };
-inline GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
+// kept_x: x is made there, of rows that were kept in 8 bits.
+inline GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act,
+                            bool kept_x = false) {
   GradSpace g{};
   const int64_t slab = slab_of(dtype);
   const int64_t size = size_of(dtype), row = padded(k, size);
   g.dz_stride = padded(n, size);
   g.laid = row != k && is_laid(m, k, n, size);
-  if (double(m) * double(g.dz_stride) * double(size) > 0x1p61) {  // (of broadcast rows: no array is)
+  const int64_t widest = kept_x ? std::max(g.dz_stride, row) : g.dz_stride;
+  if (double(m) * double(widest) * double(size) > 0x1p61) {  // (of broadcast rows: no array is)
     g.total = INT64_MAX;
     return g;
   }
   g.dz_laid = act != HG_ACT_NONE || (g.dz_stride != n && is_laid(m, k, n, size));
   g.sums = g.dz_laid ? m * g.dz_stride * size : 0;
   g.x = g.sums + align16(ceil_div<int64_t>(m, kSumRows) * n * 4);
-  g.w = g.x + (g.laid ? m * row * size : 0);
+  g.w = g.x + (g.laid || kept_x ? m * row * size : 0);
   g.parts = g.w + (g.laid ? n * row * size : 0);
   const int64_t a = parts_bytes(m, k, n, slab, false), b = parts_bytes(n, k, m, slab, true);
   g.total = g.parts + align16(a > b ? a : b);

@@ -42,6 +42,10 @@ struct Api {
   decltype(&hg_embed) embed = nullptr;
   decltype(&hg_embed_grad) embed_grad = nullptr;
   decltype(&hg_embed_grad_workspace) embed_grad_workspace = nullptr;
+  decltype(&hg_quantize) quantize = nullptr;
+  decltype(&hg_dequantize) dequantize = nullptr;
+  decltype(&hg_linear_grad_kept) linear_grad_kept = nullptr;
+  decltype(&hg_linear_grad_kept_workspace) linear_grad_kept_workspace = nullptr;
 } api;
 constexpr int kEntries = int(sizeof(Api) / sizeof(void *));
 
@@ -493,12 +497,80 @@ PyObject *embed_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
+int32_t group_of(PyObject *o) {
+  const int64_t g = integer(o);
+  if (g != 0 && g != HG_KEPT_GROUP)
+    throw Unfit("group: neither 0 (the row) nor " + std::to_string(HG_KEPT_GROUP));
+  return int32_t(g);
+}
+// The scales of rows x cols integers, contiguous: [rows], or [rows, groups].
+at::Tensor scales(PyObject *o, const char *name, int32_t group, at::Device device, int64_t rows,
+                  int64_t cols) {
+  if (!group) return vector(o, name, {at::kFloat}, device, rows);
+  const int64_t groups = (cols + group - 1) / group;
+  const at::Tensor t = matrix(o, name, {at::kFloat}, device, rows, groups);
+  return t.is_contiguous() ? t : t.contiguous();
+}
+
+// quantize(x, group) -> (q, scale)
+PyObject *quantize(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(n, 2, [&]() -> PyObject * {
+    no_gradient({args[0]});
+    const at::Tensor x = matrix(args[0], "x", kFloats);
+    const auto dev = x.device();
+    const int64_t rows = x.size(0), dim = x.size(1);
+    const int32_t group = group_of(args[1]);
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor q = make({rows, dim}, at::kChar, dev);
+    const at::Tensor scale = group ? make({rows, (dim + group - 1) / group}, at::kFloat, dev)
+                                   : make({rows}, at::kFloat, dev);
+    hg_quantize_args a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = code_of(x.scalar_type());
+    a.group = group;
+    a.x = ptr(x);
+    a.x_stride = stride(x);
+    a.q = static_cast<int8_t *>(ptr(q));
+    a.q_stride = dim;
+    a.scale = static_cast<float *>(ptr(scale));
+    return result(api.quantize(&a, current_stream(dev)), {q, scale});
+  });
+}
+
+// dequantize(q, scale, group, out_dtype) -> (x,)
+PyObject *dequantize(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(n, 4, [&]() -> PyObject * {
+    no_gradient({args[1]});
+    const at::Tensor q = matrix(args[0], "q", {at::kChar});
+    const auto dev = q.device();
+    const int64_t rows = q.size(0), dim = q.size(1);
+    const int32_t group = group_of(args[2]);
+    const at::Tensor scale = scales(args[1], "scale", group, dev, rows, dim);
+    const auto out = type_or(args[3], at::kBFloat16, "out_dtype");
+    check_float(out, "out_dtype");
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor x = make({rows, dim}, out, dev);
+    hg_dequantize_args a{};
+    a.rows = rows;
+    a.dim = dim;
+    a.dtype = code_of(out);
+    a.group = group;
+    a.q = static_cast<const int8_t *>(ptr(q));
+    a.q_stride = stride(q);
+    a.scale = static_cast<const float *>(ptr(scale));
+    a.x = ptr(x);
+    a.x_stride = dim;
+    return result(api.dequantize(&a, current_stream(dev)), {x});
+  });
+}
+
 // linear(x, w, bias, act, residual, x_scale, w_scale, out_dtype, keep_pre) -> (y, pre)
 PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> PyObject * {
     no_gradient({args[0], args[1], args[2], args[4]});
     const at::Tensor x = matrix(args[0], "x", {at::kFloat, at::kHalf, at::kBFloat16,
-                                               at::kFloat8_e4m3fn});
+                                               at::kFloat8_e4m3fn, at::kChar});
     const auto dev = x.device();
     const auto type = x.scalar_type();
     const int64_t m = x.size(0), k = x.size(1);
@@ -506,14 +578,13 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const int64_t nn = w.size(0);
     at::Tensor xs, ws;
     auto out = type;
-    if (type == at::kFloat8_e4m3fn) {
+    if (type == at::kFloat8_e4m3fn || type == at::kChar) {
       out = type_or(args[7], at::kBFloat16, "out_dtype");
       if (args[5] == Py_None || args[6] == Py_None)
         throw Unfit("8-bit operands need x_scale and w_scale");
       xs = vector(args[5], "x_scale", {at::kFloat}, dev, m);
       ws = vector(args[6], "w_scale", {at::kFloat}, dev, nn);
-      if (code_of(out) == HG_DT_NONE || out == at::kFloat8_e4m3fn)
-        throw Unfit("out_dtype: unsupported with 8-bit operands");
+      check_float(out, "out_dtype");
     } else {
       if (args[5] != Py_None || args[6] != Py_None) throw Unfit("scales are for 8-bit operands");
       if (type_or(args[7], type, "out_dtype") != type) throw Unfit("out_dtype: not x's dtype");
@@ -555,21 +626,34 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
-// linear_grad(dy, x, w, pre, act, want_dx, want_dw, want_dbias, dw_dtype) -> (dx, dw, dbias)
+// linear_grad(dy, x, w, pre, act, want_dx, want_dw, want_dbias, dw_dtype, x_scale, pre_scale,
+//   group) -> (dx, dw, dbias)
 PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  return guarded(n, 9, [&]() -> PyObject * {
-    const at::Tensor x = matrix(args[1], "x", kFloats);
+  return guarded(n, 12, [&]() -> PyObject * {
+    const bool kept_x = args[9] != Py_None, kept_pre = args[10] != Py_None;
+    const int32_t group = group_of(args[11]);
+    at::Tensor x, w, xs, ps;
+    if (kept_x) {
+      x = matrix(args[1], "x", {at::kChar});
+      w = matrix(args[2], "w", kFloats, x.device(), -1, x.size(1));
+      xs = scales(args[9], "x_scale", group, x.device(), x.size(0), x.size(1));
+    } else {
+      x = matrix(args[1], "x", kFloats);
+      w = matrix(args[2], "w", {x.scalar_type()}, x.device(), -1, x.size(1));
+    }
     const auto dev = x.device();
-    const auto type = x.scalar_type();
+    const auto type = w.scalar_type();
     const int64_t m = x.size(0), k = x.size(1);
-    const at::Tensor w = matrix(args[2], "w", {type}, dev, -1, k);
     const int64_t nn = w.size(0);
     const at::Tensor dy = matrix(args[0], "dy", {type}, dev, m, nn);
     const int32_t act = int32_t(integer(args[4]));
     at::Tensor pre;
     if (act != HG_ACT_NONE) {
       if (args[3] == Py_None) throw Unfit("an activation needs pre");
-      pre = matrix(args[3], "pre", {type}, dev, m, nn);
+      pre = matrix(args[3], "pre", {kept_pre ? at::kChar : type}, dev, m, nn);
+      if (kept_pre) ps = scales(args[10], "pre_scale", group, dev, m, nn);
+    } else if (kept_pre) {
+      throw Unfit("pre_scale: without an activation there is no pre");
     }
     const auto dw_type = type_or(args[8], type, "dw_dtype");
     if (dw_type != type && dw_type != at::kFloat)
@@ -578,9 +662,16 @@ PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor dx = truth(args[5]) ? make({m, k}, type, dev) : at::Tensor();
     const at::Tensor dw = truth(args[6]) ? make({nn, k}, dw_type, dev) : at::Tensor();
     const at::Tensor db = truth(args[7]) ? make({nn}, at::kFloat, dev) : at::Tensor();
+    const bool kept = kept_x || kept_pre;
     const at::Tensor space =
-        workspace(api.linear_grad_workspace(m, k, nn, code_of(type), act), dev);
-    hg_linear_grad_args a{};
+        workspace((kept ? api.linear_grad_kept_workspace : api.linear_grad_workspace)(
+                      m, k, nn, code_of(type), act),
+                  dev);
+    hg_linear_grad_kept_args all{};
+    hg_linear_grad_args &a = all.grad;
+    all.group = group;
+    all.x_scale = static_cast<const float *>(ptr(xs));
+    all.pre_scale = static_cast<const float *>(ptr(ps));
     a.m = m;
     a.k = k;
     a.n = nn;
@@ -602,7 +693,9 @@ PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     a.dbias = static_cast<float *>(ptr(db));
     a.workspace = ptr(space);
     a.workspace_bytes = bytes_of(space);
-    return result(api.linear_grad(&a, current_stream(dev)), {dx, dw, db});
+    const auto stream = current_stream(dev);
+    return result(kept ? api.linear_grad_kept(&all, stream) : api.linear_grad(&a, stream),
+                  {dx, dw, db});
   });
 }
 
@@ -674,6 +767,8 @@ PyMethodDef methods[] = {method<bind>("bind"),
                          method<layer_norm_grad>("layer_norm_grad"),
                          method<embed>("embed"),
                          method<embed_grad>("embed_grad"),
+                         method<quantize>("quantize"),
+                         method<dequantize>("dequantize"),
                          method<linear>("linear"),
                          method<linear_grad>("linear_grad"),
                          method<distill>("distill"),

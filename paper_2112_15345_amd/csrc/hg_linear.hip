@@ -30,6 +30,14 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 struct F8 {
   uint8_t b;
 };
+// An element of 8-bit integers, whose products are summed exactly in 32-bit integers (of at most
+// 131071 terms of up to 2^14).  The sums stay in the registers of float32 ones until they are whole.
+struct I8 {
+  int8_t b;
+};
+// Elements that come with scales.
+template <typename S>
+constexpr bool kIs8 = std::is_same_v<S, F8> || std::is_same_v<S, I8>;
 template <typename S>
 struct ComputeOf {
   typedef S T;
@@ -72,6 +80,23 @@ __device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, float) {
   for (int e = 0; e < 4; ++e)
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[e]), __uint_as_float(q[e]), c, 0, 0,
                                              0);
+  return c;
+}
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, I8) {
+  return __builtin_bit_cast(
+      f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, p),
+                                                   __builtin_bit_cast(i32x4, q),
+                                                   __builtin_bit_cast(i32x4, c), 0, 0, 0));
+}
+// Whole sums as float32 values.
+template <typename S>
+__device__ __forceinline__ f32x4 summed(f32x4 c) {
+  if constexpr (std::is_same_v<S, I8>) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = float(__float_as_int(c[e]));
+  }
   return c;
 }
 
@@ -264,7 +289,7 @@ __device__ __forceinline__ u32x4 load_piece(const Operand &O, int64_t c0, int64_
         if (k < n) e[k] = p[k];
     }
   }
-  if constexpr (sizeof(S) == 1)
+  if constexpr (std::is_same_v<S, F8>)
     return widen(__builtin_bit_cast(u32x2, e));
   else
     return __builtin_bit_cast(u32x4, e);
@@ -604,7 +629,7 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
   typedef typename ComputeOf<S>::T T;
   constexpr int WI = BI / 2, WJ = BJ / 2;  // a wavefront's part: four, 2 x 2
   constexpr int NI = WI / 16, NJ = WJ / 16;
-  constexpr bool kScaled = std::is_same_v<S, F8>;
+  constexpr bool kScaled = kIs8<S>;
   using SP = Slab<T, TP, BJ, 128>;
   using SQ = Slab<T, TQ, BI, 128>;
   constexpr int kStage = SP::kBytes + SQ::kBytes;
@@ -662,6 +687,10 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
 #pragma unroll
         for (int b = 0; b < NJ; ++b) acc[a][b] = mma(acc[a][b], fp[b][h], fq[a][h], T());
   }
+#pragma unroll
+  for (int a = 0; a < NI; ++a)
+#pragma unroll
+    for (int b = 0; b < NJ; ++b) acc[a][b] = summed<S>(acc[a][b]);
   __syncthreads();
   bool mild = true;
   if constexpr (kScaled) mild = all_mild<NI, NJ>(A.E, i0 + wi, j0 + wj);
@@ -739,7 +768,7 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
   constexpr int kWaves = kWavesI * kWavesJ;
   constexpr int WI = BI / kWavesI, WJ = BJ / kWavesJ;
   constexpr int NI = WI / 16, NJ = WJ / 16;
-  constexpr bool kScaled = std::is_same_v<S, F8>;
+  constexpr bool kScaled = kIs8<S>;
   using SP = Slab<S, TP, BJ, W>;
   using SQ = Slab<S, TQ, BI, W>;
   using LP = Stream<S, TP, BJ, W, kWaves>;
@@ -842,6 +871,10 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
             acc[a][b][e] = finite(acc[a][b][e]) ? acc[a][b][e] : again[a][b][e];
     }
   }
+#pragma unroll
+  for (int a = 0; a < NI; ++a)
+#pragma unroll
+    for (int b = 0; b < NJ; ++b) acc[a][b] = summed<S>(acc[a][b]);
   __syncthreads();
   write_out<TP, kScaled>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
@@ -964,7 +997,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
   const bool in = t < G * 32 && i < A.E.rows;
   const Columns<8> C(A.E, in ? j0 + (t & 1) * 8 : A.E.cols);
   Factor scales[8];
-  if constexpr (std::is_same_v<S, F8>) {
+  if constexpr (kIs8<S>) {
     const float by = in ? A.E.row_scale[i] : 0.0f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) scales[k] = Factor(by, C.scale[k]);
@@ -976,14 +1009,24 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
   if (C.n <= 0) return;
   float sums[1][8] = {};
   float *const v = sums[0];
-  for (int s = 0; s < kWaves; ++s)
+  if constexpr (std::is_same_v<S, I8>) {
+    int32_t whole[8] = {};
+    for (int s = 0; s < kWaves; ++s)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
+      for (int k = 0; k < 8; ++k)
+        whole[k] += __float_as_int(red[s][i >> 4][i & 15][(t & 1) * 8 + k]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = float(whole[k]);
+  } else {
+    for (int s = 0; s < kWaves; ++s)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
+  }
   if (A.E.part) {
     put<float, 8>(A.E.part, (int64_t(blockIdx.y) * A.E.rows + i) * A.E.cols + C.j, v, C.n);
     return;
   }
-  if constexpr (std::is_same_v<S, F8>) {
+  if constexpr (kIs8<S>) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = scales[k].times(v[k]);
   }
@@ -1002,9 +1045,33 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
 // sizes in bfloat16) would be a second piece of dz, and twice the time of both products.
 // A wavefront takes 64 vectors of 8 columns; the block's four take turns over the rows.
 // Place b: columns b % strips, rows b / strips; a block takes every gridDim.x-th place.
+// The values before the activation (p NULL: none), 8 of them at a time: as they were, or kept in 8 bits.
 template <typename T>
-__global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, const T *pre,
-                                            int64_t pre_stride, int32_t act, int64_t m, int64_t n,
+struct PreRows {
+  const T *p;
+  int64_t stride;
+  struct Eight {
+    Vec<T, 8> e;
+    __device__ __forceinline__ void load(const PreRows &P, int64_t i, int64_t j, int n) {
+      e.template load<Move::kStreamed>(P.p + i * P.stride + j, n);
+    }
+    __device__ __forceinline__ float value(int k) const { return float(e.e[k]); }
+  };
+};
+struct PreKept : Kept {
+  struct Eight {
+    Vec<int8_t, 8> q;
+    float s;
+    __device__ __forceinline__ void load(const PreKept &P, int64_t i, int64_t j, int n) {
+      q.load(static_cast<const int8_t *>(P.p) + i * P.stride + j, n);
+      s = P.scale_of(i, j);
+    }
+    __device__ __forceinline__ float value(int k) const { return float(q.e[k]) * s; }
+  };
+};
+template <typename T, typename Pre>
+__global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, Pre pre, int32_t act,
+                                            int64_t m, int64_t n,
                                             int64_t strips, int64_t places, T *dz, int64_t dz_stride,
                                             float *part) {
   __shared__ float red[4][64 * 8 + 8];
@@ -1018,13 +1085,14 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, cons
     constexpr int U = 4;  // rows in flight
     if (left > 0)
       for (int64_t i0 = r0 + wave; i0 < r1; i0 += 4 * U) {
-        Vec<T, 8> d[U], z[U];
+        Vec<T, 8> d[U];
+        typename Pre::Eight z[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int64_t i = i0 + 4 * u;
           if (i < r1) {
             d[u].template load<Move::kStreamed>(dy + i * dy_stride + j, left);
-            if (pre) z[u].template load<Move::kStreamed>(pre + i * pre_stride + j, left);
+            if (pre.p) z[u].load(pre, i, j, left);
           }
         }
 #pragma unroll
@@ -1036,7 +1104,7 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, cons
           for (int k = 0; k < 8; ++k) v[k] = float(d[u].e[k]);
           with_act(act, [&](auto a) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] *= act_slope<decltype(a)::value>(float(z[u].e[k]));
+            for (int k = 0; k < 8; ++k) v[k] *= act_slope<decltype(a)::value>(z[u].value(k));
           });
           if (left < 8) {
 #pragma unroll
@@ -1252,7 +1320,7 @@ hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
   E.residual_stride = A.residual_stride;
   E.pre = A.pre;
   E.pre_stride = A.pre_stride;
-  if (A.dtype == HG_DT_E4M3) {
+  if (A.dtype == HG_DT_E4M3 || A.dtype == HG_DT_I8) {
     E.row_scale = A.x_scale;
     E.col_scale = A.w_scale;
   }
@@ -1268,8 +1336,9 @@ hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
 }
 
 template <typename T>
-hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
-  const GradSpace g = grad_space(A.m, A.k, A.n, A.dtype, A.act);
+hipError_t linear_grad(const hg_linear_grad_args &A, const Kept &kept_x, const Kept &kept_pre,
+                       hipStream_t stream) {
+  const GradSpace g = grad_space(A.m, A.k, A.n, A.dtype, A.act, kept_x.p != nullptr);
   char *const ws = static_cast<char *>(A.workspace);
   Operand dz{A.dy, A.dy_stride, A.m}, dz_turned{A.dy, A.dy_stride, A.n};
   const bool has_act = A.act != HG_ACT_NONE;
@@ -1280,10 +1349,15 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
     const int64_t places = strips * chunks;
     T *const to = g.dz_laid && products ? reinterpret_cast<T *>(ws + g.dz) : nullptr;
     float *const sums = A.dbias ? reinterpret_cast<float *>(ws + g.sums) : nullptr;
-    hipLaunchKernelGGL((k_dz<T>), dim3(unsigned(std::min(places, kMostBlocks))), dim3(256), 0, stream,
-                       static_cast<const T *>(A.dy), A.dy_stride,
-                       has_act ? static_cast<const T *>(A.pre) : nullptr, A.pre_stride, A.act, A.m,
-                       A.n, strips, places, to, g.dz_stride, sums);
+    const auto launch = [&](auto pre) {
+      hipLaunchKernelGGL((k_dz<T, decltype(pre)>), dim3(unsigned(std::min(places, kMostBlocks))),
+                         dim3(256), 0, stream, static_cast<const T *>(A.dy), A.dy_stride, pre, A.act,
+                         A.m, A.n, strips, places, to, g.dz_stride, sums);
+    };
+    if (has_act && kept_pre.p)
+      launch(PreKept{kept_pre});
+    else
+      launch(PreRows<T>{has_act ? static_cast<const T *>(A.pre) : nullptr, A.pre_stride});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (to) {
@@ -1317,7 +1391,16 @@ hipError_t linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
     E.cols = A.k;
     E.dtype = A.dw_dtype;
     Operand x{A.x, A.x_stride, A.k};
-    hipError_t e = g.laid ? lay<T>(x, A.m, A.k, true, ws + g.x, stream) : hipSuccess;
+    hipError_t e = hipSuccess;
+    if (kept_x.p && A.m > 0 && A.k > 0) {
+      // what the rows stand for, in T (the products' instructions take it): a rounding more than
+      // the integers and their scales have, of 2^-9 at most where their own step is some 2^-8
+      const int64_t stride = padded(A.k, sizeof(T));
+      e = launch_dequantize(kept_x, A.m, A.k, stride, A.dtype, ws + g.x, stride, stream);
+      x = Operand{ws + g.x, stride, stride, true};
+    } else if (g.laid) {
+      e = lay<T>(x, A.m, A.k, true, ws + g.x, stream);
+    }
     return e != hipSuccess ? e : product<T, true, true>(x, dz_turned, A.m, E, parts, stream);
   }
   return hipSuccess;
@@ -1334,19 +1417,22 @@ hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream) {
     case HG_DT_F32: return linear<float>(A, stream);
     case HG_DT_F16: return linear<_Float16>(A, stream);
     case HG_DT_BF16: return linear<__bf16>(A, stream);
+    case HG_DT_I8: return linear<I8>(A, stream);
     default: return linear<F8>(A, stream);
   }
 }
 
-int64_t linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act) {
-  return grad_space(m, k, n, dtype, act).total;
+int64_t linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype, int32_t act,
+                              bool kept_x) {
+  return grad_space(m, k, n, dtype, act, kept_x).total;
 }
 
-hipError_t launch_linear_grad(const hg_linear_grad_args &A, hipStream_t stream) {
+hipError_t launch_linear_grad(const hg_linear_grad_args &A, const Kept &x, const Kept &pre,
+                              hipStream_t stream) {
   switch (A.dtype) {
-    case HG_DT_F32: return linear_grad<float>(A, stream);
-    case HG_DT_F16: return linear_grad<_Float16>(A, stream);
-    default: return linear_grad<__bf16>(A, stream);
+    case HG_DT_F32: return linear_grad<float>(A, x, pre, stream);
+    case HG_DT_F16: return linear_grad<_Float16>(A, x, pre, stream);
+    default: return linear_grad<__bf16>(A, x, pre, stream);
   }
 }
 

@@ -1,0 +1,209 @@
+// Rows kept in 8-bit integers, and what they stand for.
+//
+//   c = max(max |x| / 127, 2^-126) over a row, or over each group of 128 columns,  q = x / c rounded
+//   x = q c
+//
+// Bound by memory: 16 bytes in and 8 (4 of float32) out for a lane at a time, rows read once.
+// The quotient is the float32 one, rounded to the nearest integer, of two as near the even one: so
+// that the integers are the definition's bit for bit.  A product with 1 / c rounds to the same integer
+// unless it lies within kNear of a middle between two, and only there is it divided.
+#include "hg_rows.hpp"
+
+namespace hg {
+namespace {
+
+// |RN(x r) - RN(x / c)| for r = RN(1 / c): three roundings of 2^-24 of at most 127 each, below 2^-15.
+constexpr float kNear = 0x1p-15f;
+
+// i / per and i % per.  (The division of 64 bits takes some 100 instructions, of 32 some 20.)
+struct Place {
+  int64_t row, part;
+};
+__device__ __forceinline__ Place place_of(int64_t i, int64_t per) {
+  if ((i | per) >> 32 == 0) {
+    const uint32_t row = uint32_t(i) / uint32_t(per);
+    return Place{int64_t(row), int64_t(uint32_t(i) - row * uint32_t(per))};
+  }
+  return Place{i / per, i % per};
+}
+
+// The quotients of V values, exact to the integer they round to (none where the group is broken).
+template <int V>
+__device__ __forceinline__ void quotients(const float *x, float c, float f, float *q) {
+  float off = 0.0f;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    q[k] = x[k] * f;
+    off = fmaxf(off, fabsf(q[k] - rintf(q[k])));
+  }
+  if (off > 0.5f - kNear) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) q[k] = x[k] / c;
+  }
+}
+
+// G lanes take a group of columns: `groups` of `width` columns a row.  NV vectors a lane hold it;
+// walks over the groups, the next one's loads in flight while this one is written.
+template <typename T, int G, int NV>
+__global__ __launch_bounds__(kBlock) void k_quantize(hg_quantize_args A, int64_t groups,
+                                                     int64_t width) {
+  constexpr int V = kVec<T>;
+  constexpr int kRows = Group<G>::kRows;
+  __shared__ float red[Group<G>::kLds];
+  Group<G> grp(red);
+  const int lane = threadIdx.x % G;
+  const int64_t all = A.rows * groups, step = int64_t(gridDim.x) * kRows;
+  Vec<T> x[NV];
+  const auto load = [&](int64_t i) {
+    const Place at = place_of(i, groups);
+    const int64_t row = at.row, c0 = at.part * width;
+    const int n = int(min(width, A.dim - c0));
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * G + lane) * V;
+      if (c < n)
+        x[v].template load<Move::kStreamed>(
+            static_cast<const T *>(A.x) + row * A.x_stride + c0 + c, n - c);
+    }
+  };
+  int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / G;
+  if (i < all) load(i);
+  for (; i < all; i += step) {
+    const Place p = place_of(i, groups);
+    const int64_t row = p.row, c0 = p.part * width;
+    const int n = int(min(width, A.dim - c0));
+    float h[NV][V];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        h[v][j] = (v * G + lane) * V < n ? float(x[v].e[j]) : 0.0f;
+        amax = max(amax, mag(h[v][j]));
+      }
+    if (i + step < all) load(i + step);
+    amax = grp.max(amax);
+    const float c = scale_of<true>(amax), f = 1.0f / c;
+    if (lane == 0) A.scale[i] = c;
+    uint8_t *const q = reinterpret_cast<uint8_t *>(A.q) + row * A.q_stride + c0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int at = (v * G + lane) * V;
+      if (at < n) {
+        float t[V] = {};
+        if (!is_broken(amax)) quotients<V>(h[v], c, f, t);
+        store_i8<V>(q + at, t, n - at);
+      }
+    }
+  }
+}
+
+// Rows that do not fit in a block's registers: read twice.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_quantize_long(hg_quantize_args A) {
+  constexpr int V = kVec<T>;
+  __shared__ float red[Group<kBlock>::kLds];
+  Group<kBlock> grp(red);
+  const uint32_t dim = uint32_t(A.dim);
+  for (int64_t i = blockIdx.x; i < A.rows; i += gridDim.x) {
+    const T *const x = static_cast<const T *>(A.x) + i * A.x_stride;
+    uint8_t *const q = reinterpret_cast<uint8_t *>(A.q) + i * A.q_stride;
+    uint32_t amax = 0;
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      Vec<T> t;
+      t.load(x + c, dim - c);
+#pragma unroll
+      for (int j = 0; j < V; ++j) amax = max(amax, mag(float(t.e[j])));
+    }
+    amax = grp.max(amax);
+    const float s = scale_of<true>(amax), f = 1.0f / s;
+    if (threadIdx.x == 0) A.scale[i] = s;
+    for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
+      Vec<T> t;
+      t.load(x + c, dim - c);
+      float h[V], o[V] = {};
+#pragma unroll
+      for (int j = 0; j < V; ++j) h[j] = float(t.e[j]);
+      if (!is_broken(amax)) quotients<V>(h, s, f, o);
+      store_i8<V>(q + c, o, dim - c);
+    }
+  }
+}
+
+// 16 integers a lane of a row; zeros from column `cols` to out_cols.
+template <typename O>
+__global__ __launch_bounds__(kBlock) void k_dequantize(Kept K, int64_t rows, int64_t cols,
+                                                       int64_t out_cols, O *out, int64_t stride) {
+  constexpr int N = 16;
+  const int64_t across = (out_cols + N - 1) / N, all = rows * across;
+  for (int64_t t = int64_t(blockIdx.x) * kBlock + threadIdx.x; t < all;
+       t += int64_t(gridDim.x) * kBlock) {
+    const Place p = place_of(t, across);
+    const int64_t row = p.row, c = p.part * N;
+    float v[N];
+    K.load<N>(row, c, int(max<int64_t>(0, min<int64_t>(N, cols - c))), v);
+    Vec<O, N> o;
+#pragma unroll
+    for (int k = 0; k < N; ++k) o.e[k] = O(v[k]);
+    o.store(out + row * stride + c, int(min<int64_t>(N, out_cols - c)));
+  }
+}
+
+template <typename T>
+struct Quantize {
+  const hg_quantize_args &A;
+  hipStream_t stream;
+  template <int G, int NV>
+  hipError_t run() const {
+    if constexpr (NV == 0) {
+      hipLaunchKernelGGL((k_quantize_long<T>),
+                         dim3(unsigned(std::min<int64_t>(A.rows, 65536))), dim3(kBlock), 0, stream,
+                         A);
+    } else {
+      const int64_t groups = A.group ? ceil_div<int64_t>(A.dim, A.group) : 1;
+      const int64_t blocks = ceil_div<int64_t>(A.rows * groups, Group<G>::kRows);
+      hipLaunchKernelGGL((k_quantize<T, G, NV>), dim3(unsigned(std::min(blocks, kResident))),
+                         dim3(kBlock), 0, stream, A, groups, A.group ? A.group : A.dim);
+    }
+    return hipGetLastError();
+  }
+};
+
+template <typename T>
+hipError_t quantize(const hg_quantize_args &A, hipStream_t stream) {
+  return by_dim<T>(A.group ? std::min<int64_t>(A.group, A.dim) : A.dim, Quantize<T>{A, stream});
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const hg_quantize_args &A, hipStream_t stream) {
+  if (A.rows <= 0) return hipSuccess;
+  switch (A.dtype) {
+    case HG_DT_F32: return quantize<float>(A, stream);
+    case HG_DT_F16: return quantize<_Float16>(A, stream);
+    default: return quantize<__bf16>(A, stream);
+  }
+}
+
+hipError_t launch_dequantize(const Kept &K, int64_t rows, int64_t cols, int64_t out_cols,
+                             int32_t dtype, void *out, int64_t stride, hipStream_t stream) {
+  if (rows <= 0 || out_cols <= 0) return hipSuccess;
+  const int64_t blocks = ceil_div<int64_t>(rows * ceil_div<int64_t>(out_cols, 16), kBlock);
+  const dim3 grid(unsigned(std::min(blocks, kMostBlocks))), block(kBlock);
+  switch (dtype) {
+    case HG_DT_F32:
+      hipLaunchKernelGGL(k_dequantize<float>, grid, block, 0, stream, K, rows, cols, out_cols,
+                         static_cast<float *>(out), stride);
+      break;
+    case HG_DT_F16:
+      hipLaunchKernelGGL(k_dequantize<_Float16>, grid, block, 0, stream, K, rows, cols, out_cols,
+                         static_cast<_Float16 *>(out), stride);
+      break;
+    default:
+      hipLaunchKernelGGL(k_dequantize<__bf16>, grid, block, 0, stream, K, rows, cols, out_cols,
+                         static_cast<__bf16 *>(out), stride);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace hg

@@ -1,22 +1,32 @@
-"""Dense operators on gathered rows (include/hg.h, last section): root-mean-square
-norm, matrix product with an epilogue, distillation from a teacher's top logits,
-forward and backward.
+"""Dense operators on gathered rows (include/hg.h, last section): root-mean-square norm, layer norm,
+matrix product with an epilogue (also of 8-bit rows), embedding, distillation from a teacher's top
+logits, forward and backward, and rows kept in 8-bit integers.
 
 Argument marshalling only, in the native module.  Matrices are 2-D tensors; rows may have any stride, and
 a tensor whose columns are not contiguous is copied first.  Outputs and workspaces
 are made on `stream` (default: the current stream), where the work runs; as with any
 torch call, tensors made on another stream have to be ready, and kept until it is done.
 
-Nothing is recorded for autograd: rms_norm, linear, and distill without its gradient refuse
-(ValueError) tensors that require one, unless gradients are off (torch.no_grad(), or the
-forward of a torch.autograd.Function).  The backward passes are calls of their own; distill's
-gradient can be given to logits.backward(grad).
+Nothing is recorded for autograd: embed, the norms, linear, quantize, dequantize, and distill without
+its gradient refuse (ValueError) tensors that require one, unless gradients are off (torch.no_grad(),
+or the forward of a torch.autograd.Function); so does embed_grad of a table that it adds to.  The
+backward passes are calls of their own; distill's gradient can be given to logits.backward(grad).
 
-    y, h, scale = rms_norm(x, weight, residual=r)            # h = x + r
+    x = embed(table, ids, out_dtype=torch.bfloat16)
+    y, h, scale = rms_norm(x, weight, residual=r)            # h = x + r; layer_norm the same way
     z, pre = linear(y, w, bias=b, act="gelu", residual=h, keep_pre=True)
     loss, grad = distill(logits, top_ids, top_logits, temperature=2.0, want_grad=True)
     dx, dw, db = linear_grad(dz, y, w, pre=pre, act="gelu")
     dx, dweight = rms_norm_grad(dy, h, weight, dsum=dh)
+    embed_grad(dx, ids, nodes, scale=-rate, into=table)
+
+In 8-bit integers, and with activations that are kept in 8 bits:
+
+    q, h, c = layer_norm(x, weight, bias, residual=r, out_dtype=torch.int8)
+    z, pre = linear(q, wq, bias=b, x_scale=c, w_scale=wc)
+    y8, yc = quantize(y, group=128)
+    pre8, prec = quantize(pre, group=128)
+    dx, dw, db = linear_grad(dz, y8, w, pre=pre8, act="gelu", x_scale=yc, pre_scale=prec, group=128)
 """
 from __future__ import annotations
 
@@ -28,6 +38,7 @@ from . import HG_DT_BF16, HG_DT_F16, HG_DT_F32, HG_DT_NONE, _check, load_library
 
 HG_DT_E4M3, HG_DT_I8 = 4, 6
 HG_MAX_TOP = 1024
+HG_KEPT_GROUP = 128
 HG_ACT_NONE, HG_ACT_RELU, HG_ACT_GELU, HG_ACT_SILU = 0, 1, 2, 3
 _ACTS = {None: HG_ACT_NONE, "none": HG_ACT_NONE, "relu": HG_ACT_RELU, "gelu": HG_ACT_GELU,
          "silu": HG_ACT_SILU}
@@ -94,6 +105,20 @@ class LinearGradArgs(ctypes.Structure):
                 ("pre_stride", _I64), ("x", _P), ("x_stride", _I64), ("w", _P),
                 ("w_stride", _I64), ("dx", _P), ("dx_stride", _I64), ("dw", _P),
                 ("dw_stride", _I64), ("dbias", _P), ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class QuantizeArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I64), ("dtype", _I32), ("group", _I32), ("x", _P),
+                ("x_stride", _I64), ("q", _P), ("q_stride", _I64), ("scale", _P)]
+
+
+class DequantizeArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I64), ("dtype", _I32), ("group", _I32), ("q", _P),
+                ("q_stride", _I64), ("scale", _P), ("x", _P), ("x_stride", _I64)]
+
+
+class LinearGradKeptArgs(ctypes.Structure):
+    _fields_ = [("grad", LinearGradArgs), ("group", _I32), ("x_scale", _P), ("pre_scale", _P)]
 
 
 class DistillArgs(ctypes.Structure):
@@ -196,19 +221,35 @@ def linear(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=None,
            keep_pre: bool = False, stream=None):
     """(y, pre): y = act(x w^T + bias) + residual (hg_linear); pre: the values before the
     activation, with keep_pre (else None).  x [m, k], w [n, k]; act None, "relu", "gelu" (tanh
-    form) or "silu".  With torch.float8_e4m3fn x and w, x_scale [m] and w_scale [n] (float32)
-    are needed, and out_dtype (default bfloat16) is the type of y, pre and residual."""
+    form) or "silu".  With torch.float8_e4m3fn or torch.int8 x and w, x_scale [m] and w_scale [n]
+    (float32) are needed, and out_dtype (default bfloat16) is the type of y, pre and residual."""
     return _call("linear", stream, x, w, bias, _act(act), residual, x_scale, w_scale, out_dtype,
                  keep_pre)
 
 
 def linear_grad(dy, x, w, pre=None, act=None, want_dx: bool = True, want_dw: bool = True,
-                want_dbias: bool = True, dw_dtype=None, stream=None):
+                want_dbias: bool = True, dw_dtype=None, x_scale=None, pre_scale=None,
+                group: int = 0, stream=None):
     """(dx, dw, dbias) of linear (hg_linear_grad).  pre: the forward call's, needed with an
     activation.  dw is in dw_dtype (default w's, or float32), dbias in float32.  The gradient
-    of residual is dy.  What is not wanted is None."""
+    of residual is dy.  What is not wanted is None.
+    x or pre may be what quantize kept of it, with its x_scale or pre_scale, and the group of
+    both (hg_linear_grad_kept); x and w need not have the same type then."""
     return _call("linear_grad", stream, dy, x, w, pre, _act(act), want_dx, want_dw, want_dbias,
-                 dw_dtype)
+                 dw_dtype, x_scale, pre_scale, group)
+
+
+def quantize(x, group: int = 0, stream=None):
+    """(q, scale): x's rows in torch.int8, and what to multiply them with (hg_quantize): scale is
+    [rows], for linear's x_scale or w_scale, or with group 128 (a scale for every 128 columns, for
+    activations that are kept) [rows, ceil(dim / 128)].  A row (or group) that is not finite is
+    zeros with a scale of NaN."""
+    return _call("quantize", stream, x, group)
+
+
+def dequantize(q, scale, group: int = 0, out_dtype=torch.bfloat16, stream=None):
+    """q times scale, as quantize made them, rounded once to out_dtype (hg_dequantize)."""
+    return _call("dequantize", stream, q, scale, group, out_dtype)[0]
 
 
 def distill(logits, ids, teacher, temperature: float = 1.0, row_weight=None,
