@@ -791,7 +791,10 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
 
   bool mild = true;  // (found out here, before there is anything to wait for)
   if constexpr (kScaled) mild = all_mild<NI, NJ>(A.E, i0 + wi, j0 + wj);
-  const bool idle = i0 + wi >= A.E.rows || j0 + wj >= A.E.cols;  // no part of C for this wavefront
+  // no part of C for this wavefront (of integers it multiplies all the same: with this branch the
+  // sums were copied and spilled in the loop, 948 us for 16384 x 4096 x 4096)
+  const bool idle =
+      !std::is_same_v<S, I8> && (i0 + wi >= A.E.rows || j0 + wj >= A.E.cols);
 
   f32x4 acc[NI][NJ];
   const auto multiply_all = [&](f32x4 (&acc)[NI][NJ], auto step) {

@@ -3,16 +3,21 @@
 //   c = max(max |x| / 127, 2^-126) over a row, or over each group of 128 columns,  q = x / c rounded
 //   x = q c
 //
-// Bound by memory: 16 bytes in and 8 (4 of float32) out for a lane at a time, rows read once.
 // The quotient is the float32 one, rounded to the nearest integer, of two as near the even one: so
 // that the integers are the definition's bit for bit.  A product with 1 / c rounds to the same integer
 // unless it lies within kNear of a middle between two, and only there is it divided.
+//
+// Bound by memory once few enough instructions are left for an element (65537 x 1024 in bfloat16, in
+// groups: 67 us with 8 elements a lane, float32 maxima and a 64-bit division for each group): a lane
+// takes kWide neighbours, the largest magnitude is taken of 16-bit halves, and the position in the row
+// is counted up.
 #include "hg_rows.hpp"
 
 namespace hg {
 namespace {
 
-// |RN(x r) - RN(x / c)| for r = RN(1 / c): three roundings of 2^-24 of at most 127 each, below 2^-15.
+// Of r, a reciprocal of c within 2^-23: |RN(x r) - RN(x / c)| is at most 2^-23 + 2 x 2^-24 of 127,
+// below 2^-15.
 constexpr float kNear = 0x1p-15f;
 
 // i / per and i % per.  (The division of 64 bits takes some 100 instructions, of 32 some 20.)
@@ -27,72 +32,124 @@ __device__ __forceinline__ Place place_of(int64_t i, int64_t per) {
   return Place{i / per, i % per};
 }
 
-// The quotients of V values, exact to the integer they round to (none where the group is broken).
-template <int V>
-__device__ __forceinline__ void quotients(const float *x, float c, float f, float *q) {
+// Neighbours of a row that a lane takes: 16 bytes of integers; 8 of float32.
+template <typename T>
+constexpr int kWide = sizeof(T) == 2 ? 16 : 8;
+
+// The largest magnitude's bits as a float32's (of 16-bit types: as their own, two at a time).
+template <typename T, int N>
+__device__ __forceinline__ uint32_t largest(const Vec<T, N> &x, uint32_t before) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  uint32_t w[N * sizeof(T) / 4];
+  __builtin_memcpy(w, x.e, sizeof(w));
+#pragma unroll
+  for (int k = 0; k < int(N * sizeof(T) / 4); ++k) {
+    if constexpr (sizeof(T) == 4)
+      before = max(before, w[k] & 0x7fffffffu);
+    else
+      before = __builtin_bit_cast(
+          uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, before),
+                                              __builtin_bit_cast(u16x2, w[k] & 0x7fff7fffu)));
+  }
+  return before;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t as_f32_bits(uint32_t m) {
+  if constexpr (sizeof(T) == 4) {
+    return m;
+  } else {
+    const uint16_t top = uint16_t(max(m & 0xffffu, m >> 16));
+    return __float_as_uint(float(__builtin_bit_cast(T, top)));
+  }
+}
+
+// N (a multiple of 4) of the values as integers; zeros where the group is broken.
+template <int N>
+__device__ __forceinline__ void integers(const float *x, float c, float f, bool broken,
+                                         uint32_t *w) {
+  float q[N];
   float off = 0.0f;
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
+  for (int k = 0; k < N; ++k) {
     q[k] = x[k] * f;
     off = fmaxf(off, fabsf(q[k] - rintf(q[k])));
   }
   if (off > 0.5f - kNear) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) q[k] = x[k] / c;
+    for (int k = 0; k < N; ++k) q[k] = x[k] / c;
+  }
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k)
+    w[k] = broken ? 0 : pack_i8(q[4 * k], q[4 * k + 1], q[4 * k + 2], q[4 * k + 3]);
+}
+template <int N>
+__device__ __forceinline__ void store_words(uint8_t *p, const uint32_t *w, int n) {
+  if (n >= N) {
+    __builtin_memcpy(p, w, N);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
   }
 }
 
-// G lanes take a group of columns: `groups` of `width` columns a row.  NV vectors a lane hold it;
-// walks over the groups, the next one's loads in flight while this one is written.
+// G lanes take a group of columns: `groups` of `width` columns a row.  NV times kWide neighbours a
+// lane hold it; walks over the groups, the next one's loads in flight while this one is written.
 template <typename T, int G, int NV>
 __global__ __launch_bounds__(kBlock) void k_quantize(hg_quantize_args A, int64_t groups,
                                                      int64_t width) {
-  constexpr int V = kVec<T>;
+  constexpr int V = kWide<T>;
   constexpr int kRows = Group<G>::kRows;
   __shared__ float red[Group<G>::kLds];
   Group<G> grp(red);
   const int lane = threadIdx.x % G;
   const int64_t all = A.rows * groups, step = int64_t(gridDim.x) * kRows;
-  Vec<T> x[NV];
-  const auto load = [&](int64_t i) {
-    const Place at = place_of(i, groups);
-    const int64_t row = at.row, c0 = at.part * width;
+  const Place by = place_of(step, groups);
+  int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / G;
+  Place at = place_of(i, groups), next = at;
+  Vec<T, V> x[NV];
+  const auto load = [&](Place p) {
+    const int64_t c0 = p.part * width;
     const int n = int(min(width, A.dim - c0));
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * G + lane) * V;
       if (c < n)
-        x[v].template load<Move::kStreamed>(
-            static_cast<const T *>(A.x) + row * A.x_stride + c0 + c, n - c);
+        x[v].template load<Move::kStreamed>(static_cast<const T *>(A.x) + p.row * A.x_stride + c0 + c,
+                                            n - c);
+      else
+        __builtin_memset(x[v].e, 0, sizeof(x[v].e));
     }
   };
-  int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / G;
-  if (i < all) load(i);
-  for (; i < all; i += step) {
-    const Place p = place_of(i, groups);
-    const int64_t row = p.row, c0 = p.part * width;
+  if (i < all) load(at);
+  for (; i < all; i += step, at = next) {
+    const int64_t c0 = at.part * width;
     const int n = int(min(width, A.dim - c0));
-    float h[NV][V];
     uint32_t amax = 0;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        h[v][j] = (v * G + lane) * V < n ? float(x[v].e[j]) : 0.0f;
-        amax = max(amax, mag(h[v][j]));
-      }
-    if (i + step < all) load(i + step);
-    amax = grp.max(amax);
-    const float c = scale_of<true>(amax), f = 1.0f / c;
-    if (lane == 0) A.scale[i] = c;
-    uint8_t *const q = reinterpret_cast<uint8_t *>(A.q) + row * A.q_stride + c0;
+    Vec<T, V> now[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int at = (v * G + lane) * V;
-      if (at < n) {
-        float t[V] = {};
-        if (!is_broken(amax)) quotients<V>(h[v], c, f, t);
-        store_i8<V>(q + at, t, n - at);
+      now[v] = x[v];
+      amax = largest<T, V>(now[v], amax);
+    }
+    next = Place{at.row + by.row, at.part + by.part};
+    if (next.part >= groups) next = Place{next.row + 1, next.part - groups};
+    if (i + step < all) load(next);
+    amax = grp.max(as_f32_bits<T>(amax));
+    const bool broken = is_broken(amax);
+    const float c = scale_of<true>(amax), f = __builtin_amdgcn_rcpf(c);
+    if (lane == 0) A.scale[i] = c;
+    uint8_t *const q = reinterpret_cast<uint8_t *>(A.q) + at.row * A.q_stride + c0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int j = (v * G + lane) * V;
+      if (j < n) {
+        float h[V];
+        uint32_t w[V / 4];
+#pragma unroll
+        for (int k = 0; k < V; ++k) h[k] = float(now[v].e[k]);
+        integers<V>(h, c, f, broken, w);
+        store_words<V>(q + j, w, n - j);
       }
     }
   }
@@ -116,16 +173,17 @@ __global__ __launch_bounds__(kBlock) void k_quantize_long(hg_quantize_args A) {
       for (int j = 0; j < V; ++j) amax = max(amax, mag(float(t.e[j])));
     }
     amax = grp.max(amax);
-    const float s = scale_of<true>(amax), f = 1.0f / s;
+    const float s = scale_of<true>(amax), f = __builtin_amdgcn_rcpf(s);
     if (threadIdx.x == 0) A.scale[i] = s;
     for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
       Vec<T> t;
       t.load(x + c, dim - c);
-      float h[V], o[V] = {};
+      float h[V];
+      uint32_t w[V / 4];
 #pragma unroll
       for (int j = 0; j < V; ++j) h[j] = float(t.e[j]);
-      if (!is_broken(amax)) quotients<V>(h, s, f, o);
-      store_i8<V>(q + c, o, dim - c);
+      integers<V>(h, s, f, is_broken(amax), w);
+      store_words<V>(q + c, w, dim - c);
     }
   }
 }
@@ -171,7 +229,8 @@ struct Quantize {
 
 template <typename T>
 hipError_t quantize(const hg_quantize_args &A, hipStream_t stream) {
-  return by_dim<T>(A.group ? std::min<int64_t>(A.group, A.dim) : A.dim, Quantize<T>{A, stream});
+  const int64_t width = A.group ? std::min<int64_t>(A.group, A.dim) : A.dim;
+  return by_vectors(ceil_div<int64_t>(width, kWide<T>), Quantize<T>{A, stream});
 }
 
 }  // namespace

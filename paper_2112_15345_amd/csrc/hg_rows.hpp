@@ -110,7 +110,8 @@ template <int V>
 __device__ __forceinline__ void store_i8(uint8_t *p, const float *v, int n) {
   uint32_t w[V / 4];
 #pragma unroll
-  for (int i = 0; i < V / 4; ++i) w[i] = pack_i8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  for (int i = 0; i < V / 4; ++i)
+    w[i] = pack_i8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
   if (n >= V) {
     __builtin_memcpy(p, w, V);
   } else {
@@ -182,9 +183,8 @@ __device__ __forceinline__ void store_row(T *p, const float *v, int n) {
 }
 
 // How a row is shared: f.template run<G, NV>().
-template <typename T, typename F>
-hipError_t by_dim(int64_t dim, F f) {
-  const int64_t vecs = ceil_div<int64_t>(dim, kVec<T>);
+template <typename F>
+hipError_t by_vectors(int64_t vecs, F f) {
   if (vecs <= 8) return f.template run<8, 1>();
   if (vecs <= 16) return f.template run<16, 1>();
   if (vecs <= 32) return f.template run<32, 1>();
@@ -194,6 +194,10 @@ hipError_t by_dim(int64_t dim, F f) {
   if (vecs <= 512) return f.template run<256, 2>();
   if (vecs <= 1024) return f.template run<256, 4>();
   return f.template run<256, 0>();
+}
+template <typename T, typename F>
+hipError_t by_dim(int64_t dim, F f) {
+  return by_vectors(ceil_div<int64_t>(dim, kVec<T>), f);
 }
 
 }  // namespace
