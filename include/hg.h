@@ -758,7 +758,7 @@ typedef struct hg_embed_grad_args {
   int64_t workspace_bytes;
 } hg_embed_grad_args;
 hg_status hg_embed_grad(const hg_embed_grad_args *args, hipStream_t stream);
-int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, int32_t add);
+int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim);
 
 /* Rows in 8-bit integers, for products of integers or to keep activations in half the memory or
  * less until the backward pass.  Over each row (group 0), or over each HG_KEPT_GROUP columns of a row

@@ -172,7 +172,7 @@ def _bind(lib: ctypes.CDLL) -> ctypes.CDLL:
         "hg_layer_norm_grad_workspace": ([_I64, _I64], _I64),
         "hg_embed": ([_P, _P], _I32),
         "hg_embed_grad": ([_P, _P], _I32),
-        "hg_embed_grad_workspace": ([_I64, _I64, _I64, _I32], _I64),
+        "hg_embed_grad_workspace": ([_I64, _I64, _I64], _I64),
         "hg_quantize": ([_P, _P], _I32),
         "hg_dequantize": ([_P, _P], _I32),
         "hg_linear_grad_kept": ([_P, _P], _I32),

@@ -194,9 +194,9 @@ hg_status hg_embed(const hg_embed_args *a, hipStream_t stream) {
   return launched(launch_embed(*a, stream), "hg_embed");
 }
 
-int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, int32_t add) {
+int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim) {
   if (n <= 0 || nodes <= 0 || dim <= 0 || n >= kMost || nodes >= kMost || dim >= kMost) return 0;
-  return embed_grad_workspace(n, nodes, dim, add != 0);
+  return embed_grad_workspace(n, nodes, dim);
 }
 
 hg_status hg_embed_grad(const hg_embed_grad_args *a, hipStream_t stream) {
@@ -217,7 +217,7 @@ hg_status hg_embed_grad(const hg_embed_grad_args *a, hipStream_t stream) {
     HG_REQUIRE(in_ok(a->dy, a->dy_stride), "hg_embed_grad: dy is NULL or its stride negative");
     HG_REQUIRE(a->ids, "hg_embed_grad: ids are NULL");
     HG_REQUIRE(a->workspace && a->workspace_bytes >=
-                                   hg_embed_grad_workspace(a->n, a->nodes, a->dim, a->add),
+                                   hg_embed_grad_workspace(a->n, a->nodes, a->dim),
                "hg_embed_grad: workspace too small");
   }
   clear_pending();

@@ -32,7 +32,7 @@ hipError_t launch_layer_norm_grad(const hg_layer_norm_grad_args &A, hipStream_t 
 
 hipError_t launch_embed(const hg_embed_args &A, hipStream_t stream);
 hipError_t launch_embed_grad(const hg_embed_grad_args &A, hipStream_t stream);
-int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, bool add);
+int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim);
 
 struct Kept;
 hipError_t launch_quantize(const hg_quantize_args &A, hipStream_t stream);

@@ -230,9 +230,13 @@ inline GradSpace grad_space(int64_t m, int64_t k, int64_t n, int32_t dtype, int3
 
 // ---- the gradient of an embedding -------------------------------------------------
 
-// Ids are sorted by least significant digits first: in one block's LDS up to kSortSmall of them,
-// past that by tiles of 256 kItems, with as few digits as 11 bits each allow.
+// Ids are sorted by least significant digits first: in one block's LDS up to kSortSmall of them, past
+// that by tiles of as many, with as few digits as 11 bits each allow.  Up to kFewTiles tiles each
+// finds by itself what the others have of a digit; past that a kernel of its own does (a launch
+// more of each pass, some 5 us).
 constexpr int64_t kSortSmall = 4096;
+constexpr int64_t kSortTile = 4096;
+constexpr int64_t kFewTiles = 64;
 constexpr int kMostDigitBits = 11;
 constexpr int kSmallDigitBits = 8;
 
@@ -241,30 +245,29 @@ constexpr int kSmallDigitBits = 8;
 struct EmbedPlan {
   int bits, passes, digit;  // of the ids, of the sort, of a pass
   bool small;
-  int64_t tiles, tile;
+  int64_t tiles;
   int64_t chunk, chunks;
-  int64_t pairs, other, counts, totals, marks, parts, total;  // byte offsets in the workspace
+  int64_t pairs, other, counts, totals, ends, parts, total;  // byte offsets in the workspace
 };
-inline EmbedPlan embed_plan(int64_t n, int64_t nodes, int64_t dim, bool add) {
+inline EmbedPlan embed_plan(int64_t n, int64_t nodes, int64_t dim) {
   EmbedPlan p{};
   while (p.bits < 32 && (nodes >> p.bits) > 0) ++p.bits;  // (ids that count for nothing are `nodes`)
   p.small = n <= kSortSmall;
   const int most = p.small ? kSmallDigitBits : kMostDigitBits;
   p.passes = (p.bits + most - 1) / most;
   p.digit = (p.bits + p.passes - 1) / p.passes;
-  p.tile = n <= int64_t(1) << 18 ? 1024 : 4096;
-  p.tiles = ceil_div<int64_t>(n, p.tile);
-  // chunks that fill the units: long ones leave fewer parts, short ones are done sooner
+  p.tiles = ceil_div<int64_t>(n, kSortTile);
+  // chunks that fill the units, as long as they can be for that: each leaves up to two parts
   p.chunk = 8;
-  while (p.chunk < 64 && n * ceil_div<int64_t>(dim, 1024) > p.chunk * 2048) p.chunk *= 2;
+  while (p.chunk < 64 && n * std::min<int64_t>(dim, 2048) > (p.chunk << 21)) p.chunk *= 2;
   p.chunks = ceil_div<int64_t>(n, p.chunk);
   const int64_t bins = int64_t(1) << p.digit;
   p.pairs = 0;
   p.other = p.pairs + align16(n * 8);
   p.counts = p.other + (p.small ? 0 : align16(n * 8));
   p.totals = p.counts + (p.small ? 0 : align16(bins * p.tiles * 4));
-  p.marks = p.totals + (p.small ? 0 : align16(bins * 4));
-  p.parts = p.marks + (add ? 0 : align16(nodes));
+  p.ends = p.totals + (p.small ? 0 : align16(bins * 4));
+  p.parts = p.ends + align16(p.chunks * 4);
   p.total = p.parts + 2 * p.chunks * dim * 4;
   return p;
 }

@@ -474,7 +474,7 @@ PyObject *embed_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
       d = make({nodes, dim}, out, dev);
     }
     const at::Tensor ws =
-        workspace(api.embed_grad_workspace(rows, nodes, dim, add), dev);
+        workspace(api.embed_grad_workspace(rows, nodes, dim), dev);
     hg_embed_grad_args a{};
     a.n = rows;
     a.nodes = nodes;

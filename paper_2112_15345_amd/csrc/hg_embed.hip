@@ -86,12 +86,12 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool in
 
 // How many of this wavefront's pairs before this one have its digit; count [digits] holds those of
 // the rounds before, and then of this one too.
-__device__ __forceinline__ uint32_t take_place(uint32_t *count, uint32_t digit, int bits, bool in) {
+__device__ __forceinline__ uint32_t take_place(uint16_t *count, uint32_t digit, int bits, bool in) {
   const uint64_t same = same_digit(digit, bits, in);
   const uint32_t before = __popcll(same & lanes_below());
   const uint32_t seen = in ? count[digit] : 0;
   wave_sync();
-  if (in && before == 0) count[digit] = seen + __popcll(same);
+  if (in && before == 0) count[digit] = uint16_t(seen + __popcll(same));
   wave_sync();
   return seen + before;
 }
@@ -118,91 +118,113 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *red, uint32
   return before + s - v;
 }
 
-// Marks of the ids that are there, cleared by `threads` threads of which this is `t`.
-__device__ __forceinline__ void clear(uint8_t *marks, int64_t nodes, int64_t t, int64_t threads) {
-  const u32x4 none = {0, 0, 0, 0};
-  for (int64_t v = t * 16; v < nodes; v += threads * 16)
-    *reinterpret_cast<u32x4 *>(marks + v) = none;  // (whole pieces: the array ends at one)
+// Zeros into a table's rows: pieces of some 64 KB, of which a launch takes those from `first` on in
+// the blocks past `own`.  The sort's kernels wait for their loads and leave the memory idle, so
+// they carry this on the side (the sums are written after them, over the zeros).
+struct Fill {
+  void *out;
+  int64_t stride, rows, dim;
+  int32_t size;  // bytes of an element
+  int64_t rows_of_piece, first, own;
+};
+// Whether this block fills.
+__device__ __forceinline__ bool filled(const Fill &F) {
+  if (int64_t(blockIdx.x) < F.own) return false;
+  const int64_t r0 = (F.first + blockIdx.x - F.own) * F.rows_of_piece;
+  const uint32_t rows = uint32_t(min(F.rows_of_piece, F.rows - r0));
+  const int64_t bytes = F.dim * F.size;
+  const uint32_t across = uint32_t((bytes + 15) / 16);
+  for (uint64_t t = threadIdx.x; t < uint64_t(rows) * across; t += blockDim.x) {
+    const uint32_t r = uint32_t(t) / across;  // (either there is one row, or t is small)
+    const int64_t row = rows == 1 ? 0 : r;
+    const int64_t c = (int64_t(t) - row * across) * 16;
+    Vec<uint8_t, 16> none;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) none.e[k] = 0;
+    none.template store<Move::kStreamed>(
+        static_cast<uint8_t *>(F.out) + (r0 + row) * F.stride * F.size + c,
+        int(min<int64_t>(16, bytes - c)));
+  }
+  return true;
 }
 
 // All of the sort in one block's LDS.
-constexpr int kSmallThreads = 1024;
-__global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int64_t *ids, int32_t n,
-                                                              int64_t nodes, int32_t passes,
-                                                              int32_t digit, Pair *out,
-                                                              uint8_t *marks) {
-  constexpr int kWaves = kSmallThreads / 64, kRounds = int(kSortSmall) / kSmallThreads;
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kSortRounds = int(kSortTile) / kSortThreads;
+static_assert(kSortSmall == kSortTile, "as many pairs a thread");
+__global__ __launch_bounds__(kSortThreads) void k_sort_small(const int64_t *ids, int32_t n,
+                                                             int64_t nodes, int32_t passes,
+                                                             int32_t digit, Pair *out, Fill fill) {
   constexpr int kBins = 1 << kSmallDigitBits;
   __shared__ Pair pairs[kSortSmall];
-  __shared__ uint32_t count[kWaves][kBins];
-  __shared__ uint32_t red[kWaves];
+  __shared__ uint16_t count[kSortWaves][kBins];
+  __shared__ uint32_t base[kBins];
+  __shared__ uint32_t red[kSortWaves];
+  if (filled(fill)) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int rounds = (n + kSmallThreads - 1) / kSmallThreads;
+  const int rounds = (n + kSortThreads - 1) / kSortThreads;
   const int first = wave * rounds * 64 + lane;
-  if (marks) clear(marks, nodes, threadIdx.x, kSmallThreads);
-  Pair p[kRounds];
+  Pair p[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
+  for (int r = 0; r < kSortRounds; ++r) {
     const int i = first + r * 64;
     p[r] = r < rounds && i < n ? pair_of(ids, i, nodes) : Pair{0, 0};
   }
-  __syncthreads();
-  if (marks) {
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-      if (r < rounds && first + r * 64 < n && p[r].id < nodes) marks[p[r].id] = 1;
-  }
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * digit;
-    for (int t = threadIdx.x; t < kWaves * kBins; t += kSmallThreads) (&count[0][0])[t] = 0;
+    const auto digit_of = [&](Pair q) { return q.id >> shift & ((1u << digit) - 1); };
+    for (int t = threadIdx.x; t < kSortWaves * kBins; t += kSortThreads) (&count[0][0])[t] = 0;
     __syncthreads();
-    uint32_t place[kRounds];
+    uint32_t place[kSortRounds];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < kSortRounds; ++r) {
       if (r < rounds)
-        place[r] = take_place(count[wave], p[r].id >> shift & ((1u << digit) - 1), digit,
-                              first + r * 64 < n);
+        place[r] = take_place(count[wave], digit_of(p[r]), digit, first + r * 64 < n);
     }
     __syncthreads();
     // a digit's pairs of all wavefronts, then the digits before it
     uint32_t sum = 0, all;
     const int d = threadIdx.x;
     if (d < kBins)
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < kSortWaves; ++w) {
         const uint32_t c = count[w][d];
-        count[w][d] = sum;
+        count[w][d] = uint16_t(sum);
         sum += c;
       }
-    const uint32_t before = block_scan<kSmallThreads>(d < kBins ? sum : 0, red, &all);
-    if (d < kBins)
-      for (int w = 0; w < kWaves; ++w) count[w][d] += before;
+    const uint32_t before = block_scan<kSortThreads>(d < kBins ? sum : 0, red, &all);
+    if (d < kBins) base[d] = before;
     __syncthreads();
     const bool last = pass + 1 == passes;
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r)
+    for (int r = 0; r < kSortRounds; ++r)
       if (r < rounds && first + r * 64 < n) {
-        const uint32_t to = count[wave][p[r].id >> shift & ((1u << digit) - 1)] + place[r];
-        (last ? out : pairs)[to] = p[r];
+        const uint32_t to = base[digit_of(p[r])] + count[wave][digit_of(p[r])] + place[r];
+        if (last)
+          out[to] = p[r];
+        else
+          pairs[to] = p[r];
       }
     if (last) return;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r)
+    for (int r = 0; r < kSortRounds; ++r)
       if (r < rounds && first + r * 64 < n) p[r] = pairs[first + r * 64];
   }
 }
 
-// A pass of the sort over more pairs: counts by tile, their sums, the pairs to their places.
-// The first pass takes them from the ids.
+// A pass of the sort over more pairs: counts by tile, then the pairs to their places.  The first
+// pass takes them from the ids.
 struct SortPass {
   const int64_t *ids;  // or
   const Pair *from;
   Pair *to;
   int64_t n, nodes, tiles;
   int32_t shift, digit;
-  uint32_t *counts;  // [digits, tiles]
-  uint32_t *totals;  // [digits]
-  uint8_t *marks;    // with ids
+  uint32_t *counts;  // of tile t and digit d at t by_tile + d by_digit
+  int64_t by_tile, by_digit;
+  uint32_t *totals;  // [digits], with k_sort_scan; else NULL
+  Fill fill;
   __device__ __forceinline__ Pair at(int64_t i) const {
     return ids ? pair_of(ids, i, nodes) : from[i];
   }
@@ -211,26 +233,29 @@ struct SortPass {
   }
 };
 
-template <int kItems>
-__global__ __launch_bounds__(kBlock) void k_sort_count(SortPass A) {
+__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortPass A) {
   __shared__ uint32_t count[1 << kMostDigitBits];
+  if (filled(A.fill)) return;
   const int bins = 1 << A.digit;
-  for (int d = threadIdx.x; d < bins; d += kBlock) count[d] = 0;
-  if (A.ids && A.marks)
-    clear(A.marks, A.nodes, int64_t(blockIdx.x) * kBlock + threadIdx.x, int64_t(gridDim.x) * kBlock);
-  __syncthreads();
-  const int64_t first = int64_t(blockIdx.x) * kBlock * kItems + threadIdx.x;
+  const int64_t first = int64_t(blockIdx.x) * kSortTile + threadIdx.x;
+  Pair p[kSortRounds];
 #pragma unroll
-  for (int u = 0; u < kItems; ++u)
-    if (first + u * kBlock < A.n) atomicAdd(&count[A.digit_of(A.at(first + u * kBlock))], 1u);
+  for (int u = 0; u < kSortRounds; ++u)
+    if (first + u * kSortThreads < A.n) p[u] = A.at(first + u * kSortThreads);
+  for (int d = threadIdx.x; d < bins; d += kSortThreads) count[d] = 0;
   __syncthreads();
-  for (int d = threadIdx.x; d < bins; d += kBlock) A.counts[d * A.tiles + blockIdx.x] = count[d];
+#pragma unroll
+  for (int u = 0; u < kSortRounds; ++u)
+    if (first + u * kSortThreads < A.n) atomicAdd(&count[A.digit_of(p[u])], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < bins; d += kSortThreads)
+    A.counts[blockIdx.x * A.by_tile + d * A.by_digit] = count[d];
 }
 
 // A block for each digit: what the tiles before have of it.
 __global__ __launch_bounds__(kBlock) void k_sort_scan(SortPass A) {
   __shared__ uint32_t red[kBlock / 64];
-  uint32_t *const row = A.counts + blockIdx.x * A.tiles;
+  uint32_t *const row = A.counts + blockIdx.x * A.by_digit;  // (by_tile is 1)
   uint32_t before = 0;
   for (int64_t t = threadIdx.x; t - threadIdx.x < A.tiles; t += kBlock) {
     uint32_t all;
@@ -242,51 +267,67 @@ __global__ __launch_bounds__(kBlock) void k_sort_scan(SortPass A) {
   if (threadIdx.x == 0) A.totals[blockIdx.x] = before;
 }
 
-template <int kItems>
-__global__ __launch_bounds__(kBlock) void k_sort_place(SortPass A) {
-  constexpr int kWaves = kBlock / 64, kBins = 1 << kMostDigitBits;
-  __shared__ uint32_t count[kWaves][kBins];
-  __shared__ uint32_t red[kWaves];
+__global__ __launch_bounds__(kSortThreads) void k_sort_place(SortPass A) {
+  constexpr int kBins = 1 << kMostDigitBits;
+  __shared__ uint16_t count[kSortWaves][kBins];
+  __shared__ uint32_t base[kBins];
+  __shared__ uint32_t red[kSortWaves];
+  if (filled(A.fill)) return;
   const int bins = 1 << A.digit;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int w = 0; w < kWaves; ++w)
-    for (int d = threadIdx.x; d < bins; d += kBlock) count[w][d] = 0;
-  const int64_t first = (int64_t(blockIdx.x) * kWaves + wave) * kItems * 64 + lane;
-  Pair p[kItems];
+  const int64_t first = (int64_t(blockIdx.x) * kSortWaves + wave) * kSortRounds * 64 + lane;
+  Pair p[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < kItems; ++r)
+  for (int r = 0; r < kSortRounds; ++r)
     p[r] = first + r * 64 < A.n ? A.at(first + r * 64) : Pair{0, 0};
-  __syncthreads();
-  uint32_t place[kItems];
-#pragma unroll
-  for (int r = 0; r < kItems; ++r)
-    place[r] = take_place(count[wave], A.digit_of(p[r]), A.digit, first + r * 64 < A.n);
-  if (A.ids && A.marks) {
-#pragma unroll
-    for (int r = 0; r < kItems; ++r)
-      if (first + r * 64 < A.n && p[r].id < A.nodes) A.marks[p[r].id] = 1;
-  }
-  // the pairs of smaller digits, those of earlier tiles, those of earlier wavefronts
+  for (int d = 2 * lane; d < bins; d += 128) *reinterpret_cast<uint32_t *>(&count[wave][d]) = 0;
+  // the pairs of smaller digits, and those of this one in earlier tiles
   uint32_t smaller = 0;
-  for (int d0 = 0; d0 < bins; d0 += kBlock) {
+  for (int d0 = 0; d0 < bins; d0 += kSortThreads) {
     const int d = d0 + threadIdx.x;
-    uint32_t all;
-    const uint32_t s = block_scan<kBlock>(d < bins ? A.totals[d] : 0, red, &all);
+    uint32_t earlier = 0, total = 0, all;
     if (d < bins) {
-      uint32_t at = smaller + s + A.counts[d * A.tiles + blockIdx.x];
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const uint32_t c = count[w][d];
-        count[w][d] = at;
-        at += c;
+      if (A.totals) {
+        earlier = A.counts[blockIdx.x * A.by_tile + d * A.by_digit];
+        total = A.totals[d];
+      } else {
+        // (loads of tiles that are not there, to have 32 at once, cost more: 15.2 us a pass of 37
+        // tiles, not 12.4)
+#pragma unroll 16
+        for (int t = 0; t < int(A.tiles); ++t) {
+          const uint32_t c = A.counts[t * A.by_tile + d * A.by_digit];
+          earlier += t < int(blockIdx.x) ? c : 0;
+          total += c;
+        }
       }
     }
+    const uint32_t s = block_scan<kSortThreads>(total, red, &all);  // (a barrier at least)
+    if (d < bins) base[d] = smaller + s + earlier;
     smaller += all;
+  }
+  uint32_t place[kSortRounds];
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r)
+    place[r] = take_place(count[wave], A.digit_of(p[r]), A.digit, first + r * 64 < A.n);
+  __syncthreads();
+  // those of earlier wavefronts
+  for (int d = threadIdx.x; d < bins; d += kSortThreads) {
+    uint32_t c[kSortWaves], sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) c[w] = count[w][d];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      count[w][d] = uint16_t(sum);
+      sum += c[w];
+    }
   }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kItems; ++r)
-    if (first + r * 64 < A.n) A.to[count[wave][A.digit_of(p[r])] + place[r]] = p[r];
+  for (int r = 0; r < kSortRounds; ++r)
+    if (first + r * 64 < A.n) {
+      const uint32_t d = A.digit_of(p[r]);
+      A.to[base[d] + count[wave][d] + place[r]] = p[r];
+    }
 }
 
 // ---- the sums ------------------------------------------------------------------
@@ -301,104 +342,130 @@ struct Sums {
   float scale;
   int64_t chunk, chunks;
   float *parts;  // [chunks, 2, dim]: of the run that came into a chunk, of the one that starts there
-  int64_t slices, sum_blocks, blocks;
-  const uint8_t *marks;  // NULL: no row is there
-  int64_t fill_rows;     // of a block that fills
+  int32_t *ends;  // [chunks]: the last chunk of the run that starts there and goes on, or 0
+  int64_t slices, blocks;
   __device__ __forceinline__ uint32_t id(int64_t i) const { return pairs[i].id; }
 };
 
-// N sums to a row of the table, n of them in it.
+template <typename O, int N>
+__device__ __forceinline__ O *row_at(const Sums &A, uint32_t row, int64_t c) {
+  return static_cast<O *>(A.out) + int64_t(row) * A.out_stride + c;
+}
+// A pair; uniform: the same for all lanes of a wavefront, by the scalar unit (nothing writes pairs in
+// the kernels that read them so).
+template <bool kUniform>
+__device__ __forceinline__ Pair pair_at(const Sums &A, int64_t i) {
+  if constexpr (kUniform) {
+    typedef const __attribute__((address_space(4))) uint64_t Word;
+    const uint64_t w = ((Word *)(A.pairs))[i];
+    return Pair{uint32_t(w), uint32_t(w >> 32)};
+  } else {
+    return A.pairs[i];
+  }
+}
+
+// N sums to a row of the table, n of them in it; `old` (kAdd): what it has.
 template <typename O, bool kAdd, int N>
 __device__ __forceinline__ void put_row(const Sums &A, uint32_t row, int64_t c, const float *v,
-                                        int n) {
-  O *const to = static_cast<O *>(A.out) + int64_t(row) * A.out_stride + c;
+                                        int n, const Vec<O, N> &old) {
   Vec<O, N> t;
-  if (kAdd) t.load(to, n);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const float s = v[k] * A.scale;
-    t.e[k] = O(kAdd ? float(t.e[k]) + s : s);
+    t.e[k] = O(kAdd ? float(old.e[k]) + s : s);
   }
-  t.store(to, n);
+  t.template store<Move::kStreamed>(row_at<O, N>(A, row, c), n);
 }
 
-// G lanes sum a chunk, for G V columns.  Blocks past sum_blocks fill rows that no id names.
+// The last chunk that a run which goes past the end of `chunk` comes into: doubled steps, then
+// halved ones.
+__device__ __forceinline__ int64_t end_of_run(const Sums &A, int64_t chunk, uint32_t run) {
+  int64_t last = chunk + 1, step = 1;
+  while (last + step < A.chunks && A.id((last + step) * A.chunk) == run) {
+    last += step;
+    step *= 2;
+  }
+  for (; step > 0; step /= 2)
+    if (last + step < A.chunks && A.id((last + step) * A.chunk) == run) last += step;
+  return last;
+}
+
+// G lanes sum a chunk, for G V columns.  (16 bytes of dy a lane: with 16 bytes of a wider result a
+// lane instead, 8 of dy, the text's gradient of 50001 x 1024 took 97 us here, not 49.)
 template <typename T, typename O, bool kAdd, int G>
 __global__ __launch_bounds__(kBlock) void k_embed_sum(Sums A) {
   constexpr int V = kVec<T>, kAhead = 8;
   for (int64_t b = blockIdx.x; b < A.blocks; b += gridDim.x) {
-    if (b >= A.sum_blocks) {
-      if constexpr (!kAdd) {
-        constexpr int W = kVec<O>;
-        const int64_t r0 = (b - A.sum_blocks) * A.fill_rows;
-        const uint32_t rows = uint32_t(min(A.fill_rows, A.nodes - r0));
-        const uint32_t across = uint32_t((A.dim + W - 1) / W);
-        Vec<O> none;
-#pragma unroll
-        for (int k = 0; k < W; ++k) none.e[k] = O(0.0f);
-        for (uint64_t t = threadIdx.x; t < uint64_t(rows) * across; t += kBlock) {
-          const int64_t r = r0 + int64_t(t / across), c = int64_t(t % across) * W;
-          if (A.marks && A.marks[r]) continue;
-          none.template store<Move::kStreamed>(static_cast<O *>(A.out) + r * A.out_stride + c,
-                                               int(min<int64_t>(W, A.dim - c)));
-        }
-      }
-      continue;
-    }
-    const int64_t chunk = b / A.slices * (kBlock / G) + threadIdx.x / G;
+    int64_t chunk = b / A.slices * (kBlock / G) + threadIdx.x / G;
+    // (the same for a wavefront's lanes: the pairs are read once for all of them)
+    if (G >= 64) chunk = int64_t(__builtin_amdgcn_readfirstlane(int(chunk)));
     const int64_t c = (b % A.slices * G + threadIdx.x % G) * V;
     if (chunk >= A.chunks || c >= A.dim) continue;
     const int n = int(min<int64_t>(V, A.dim - c));
     const int64_t first = chunk * A.chunk, last = min(first + A.chunk, A.n);
-    const uint32_t before = first > 0 ? A.id(first - 1) : ~0u;
-    const uint32_t after = last < A.n ? A.id(last) : ~0u;
-    uint32_t now = A.id(first);
+    const uint32_t before = first > 0 ? pair_at<(G >= 64)>(A, first - 1).id : ~0u;
+    const uint32_t after = last < A.n ? pair_at<(G >= 64)>(A, last).id : ~0u;
+    uint32_t now = pair_at<(G >= 64)>(A, first).id;
     float s[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) s[k] = 0.0f;
-    const auto part = [&](int which) {
-      Vec<float, V> t;
-#pragma unroll
-      for (int k = 0; k < V; ++k) t.e[k] = s[k];
-      t.store(A.parts + (2 * chunk + which) * A.dim + c, n);
-    };
+    Vec<O, V> old;
     const auto leave = [&](bool ends) {
       if (now >= A.nodes) return;
-      if (now == before)
-        part(0);
-      else if (!ends)
-        part(1);
-      else
-        put_row<O, kAdd, V>(A, now, c, s, n);
+      if (now == before || !ends) {
+        Vec<float, V> t;
+#pragma unroll
+        for (int k = 0; k < V; ++k) t.e[k] = s[k];
+        t.store(A.parts + (2 * chunk + (now != before)) * A.dim + c, n);
+      } else {
+        put_row<O, kAdd, V>(A, now, c, s, n, old);
+      }
     };
+    // pairs are read one round ahead of the rows that they name
+    Pair p[kAhead + 1];
+    const auto read = [&](int64_t e) {
+#pragma unroll
+      for (int u = 0; u <= kAhead; ++u)
+        p[u] = e + u < last ? pair_at<(G >= 64)>(A, e + u) : Pair{uint32_t(A.nodes), 0};
+    };
+    read(first);
     for (int64_t e = first; e < last; e += kAhead) {
-      Pair p[kAhead];
+      uint32_t id[kAhead];
       Vec<T> r[kAhead];
+      Vec<O, V> t[kAdd ? kAhead : 1];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        p[u] = e + u < last ? A.pairs[e + u] : Pair{uint32_t(A.nodes), 0};
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (p[u].id < A.nodes)
+      for (int u = 0; u < kAhead; ++u) {
+        id[u] = p[u].id;
+        if (id[u] < A.nodes) {
           r[u].template load<Move::kStreamed>(
               static_cast<const T *>(A.dy) + int64_t(p[u].at) * A.dy_stride + c, n);
+          // the row that a run's sum is added to, where it ends: loaded with the others (150001
+          // rows of 128 floats: 87 us where each waited for its own, now 51)
+          if (kAdd && id[u] != p[u + 1].id) t[kAdd ? u : 0].load(row_at<O, V>(A, id[u], c), n);
+        }
+      }
+      if (e + kAhead < last) read(e + kAhead);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         if (e + u < last) {
-          if (p[u].id != now) {
+          if (id[u] != now) {
             leave(true);
-            now = p[u].id;
+            now = id[u];
 #pragma unroll
             for (int k = 0; k < V; ++k) s[k] = 0.0f;
           }
           if (now < A.nodes) {
 #pragma unroll
             for (int k = 0; k < V; ++k) s[k] += float(r[u].e[k]);
+            if constexpr (kAdd) old = t[u];
           }
         }
       }
     }
     leave(now != after);
+    if (c == 0)
+      A.ends[chunk] = now < A.nodes && now == after && now != before
+                          ? int32_t(end_of_run(A, chunk, now)) : 0;
   }
 }
 
@@ -412,19 +479,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(Sums A, int64_t places) {
   const int64_t slices = (A.dim + 127) / 128;
   for (int64_t b = blockIdx.x; b < places; b += gridDim.x) {
     const int64_t chunk = b / slices;
-    // (what leaves a place is the same for the whole block)
-    const int64_t next = (chunk + 1) * A.chunk;
-    const uint32_t run = A.id(next - 1);
-    if (run >= A.nodes || A.id(next) != run) continue;
-    if (chunk > 0 && A.id(chunk * A.chunk - 1) == run) continue;
-    // the last chunk that it comes into: doubled steps, then halved ones
-    int64_t last = chunk + 1, step = 1;
-    while (last + step < A.chunks && A.id((last + step) * A.chunk) == run) {
-      last += step;
-      step *= 2;
-    }
-    for (; step > 0; step /= 2)
-      if (last + step < A.chunks && A.id((last + step) * A.chunk) == run) last += step;
+    const int64_t last = A.ends[chunk];
+    if (last == 0) continue;  // (the same for the whole block)
+    const uint32_t run = A.id((chunk + 1) * A.chunk);
     const int64_t c = (b % slices * 32 + lane) * N;
     const int n = int(max<int64_t>(0, min<int64_t>(N, A.dim - c)));
     float s[N] = {};
@@ -446,7 +503,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(Sums A, int64_t places) {
       for (int t = 1; t < kDown; ++t)
 #pragma unroll
         for (int j = 0; j < N; ++j) s[j] += red[t][lane][j];
-      put_row<O, kAdd, N>(A, run, c, s, n);
+      Vec<O, N> old;
+      if (kAdd) old.load(row_at<O, N>(A, run, c), n);
+      put_row<O, kAdd, N>(A, run, c, s, n, old);
     }
   }
 }
@@ -471,14 +530,24 @@ hipError_t forward(const hg_embed_args &A, hipStream_t stream) {
   }
 }
 
-hipError_t sort(const hg_embed_grad_args &A, const EmbedPlan &p, hipStream_t stream,
-                const Pair **sorted) {
+// Sorts the pairs; the sort's kernels take turns with the pieces to fill.
+hipError_t sort(const hg_embed_grad_args &A, const EmbedPlan &p, Fill fill, int64_t pieces,
+                hipStream_t stream, const Pair **sorted) {
   char *const ws = static_cast<char *>(A.workspace);
   Pair *to = reinterpret_cast<Pair *>(ws + p.pairs), *other = reinterpret_cast<Pair *>(ws + p.other);
-  uint8_t *const marks = A.add ? nullptr : reinterpret_cast<uint8_t *>(ws + p.marks);
+  const bool few = p.tiles <= kFewTiles;
+  int64_t launches = p.small ? 1 : 2 * p.passes;
+  // blocks of a launch that has `own` for itself
+  const auto grid = [&](int64_t own) {
+    const int64_t share = ceil_div<int64_t>(pieces - fill.first, launches--);
+    fill.own = own;
+    return dim3(unsigned(own + share));
+  };
+  const auto next = [&](dim3 g) { fill.first += g.x - fill.own; };
   if (p.small) {
-    hipLaunchKernelGGL(k_sort_small, dim3(1), dim3(kSmallThreads), 0, stream, A.ids, int32_t(A.n),
-                       A.nodes, p.passes, p.digit, to, marks);
+    const dim3 g = grid(1);
+    hipLaunchKernelGGL(k_sort_small, g, dim3(kSortThreads), 0, stream, A.ids, int32_t(A.n), A.nodes,
+                       p.passes, p.digit, to, fill);
     *sorted = to;
     return hipGetLastError();
   }
@@ -489,21 +558,21 @@ hipError_t sort(const hg_embed_grad_args &A, const EmbedPlan &p, hipStream_t str
   S.tiles = p.tiles;
   S.digit = p.digit;
   S.counts = reinterpret_cast<uint32_t *>(ws + p.counts);
-  S.totals = reinterpret_cast<uint32_t *>(ws + p.totals);
-  S.marks = marks;
-  const dim3 tiles(unsigned(p.tiles)), block(kBlock);
+  S.by_tile = few ? int64_t(1) << p.digit : 1;
+  S.by_digit = few ? 1 : p.tiles;
+  S.totals = few ? nullptr : reinterpret_cast<uint32_t *>(ws + p.totals);
   for (int pass = 0; pass < p.passes; ++pass) {
     S.shift = pass * p.digit;
     S.to = to;
-    if (p.tile == 1024)
-      hipLaunchKernelGGL(k_sort_count<4>, tiles, block, 0, stream, S);
-    else
-      hipLaunchKernelGGL(k_sort_count<16>, tiles, block, 0, stream, S);
-    hipLaunchKernelGGL(k_sort_scan, dim3(1u << p.digit), block, 0, stream, S);
-    if (p.tile == 1024)
-      hipLaunchKernelGGL(k_sort_place<4>, tiles, block, 0, stream, S);
-    else
-      hipLaunchKernelGGL(k_sort_place<16>, tiles, block, 0, stream, S);
+    dim3 g = grid(p.tiles);
+    S.fill = fill;
+    hipLaunchKernelGGL(k_sort_count, g, dim3(kSortThreads), 0, stream, S);
+    next(g);
+    if (!few) hipLaunchKernelGGL(k_sort_scan, dim3(1u << p.digit), dim3(kBlock), 0, stream, S);
+    g = grid(p.tiles);
+    S.fill = fill;
+    hipLaunchKernelGGL(k_sort_place, g, dim3(kSortThreads), 0, stream, S);
+    next(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     S.ids = nullptr;
@@ -514,15 +583,28 @@ hipError_t sort(const hg_embed_grad_args &A, const EmbedPlan &p, hipStream_t str
   return hipSuccess;
 }
 
+// Zeros alone.
+__global__ __launch_bounds__(kBlock) void k_fill(Fill fill) { filled(fill); }
+
 template <typename T, typename O, bool kAdd>
 hipError_t gradient(const hg_embed_grad_args &A, hipStream_t stream) {
-  const EmbedPlan p = embed_plan(A.n, A.nodes, A.dim, kAdd);
-  Sums S{};
-  if (A.n > 0) {
-    const hipError_t e = sort(A, p, stream, &S.pairs);
-    if (e != hipSuccess) return e;
+  Fill fill{A.dtable, A.dtable_stride, A.nodes, A.dim, int32_t(sizeof(O)), 0, 0, 0};
+  fill.rows_of_piece = std::max<int64_t>(1, 65536 / (A.dim * int64_t(sizeof(O))));
+  // (a launch has fewer than 2^32 threads, of 1024 in a block)
+  const int64_t most = int64_t(1) << 21;
+  if (ceil_div<int64_t>(A.nodes, fill.rows_of_piece) > most)
+    fill.rows_of_piece = ceil_div<int64_t>(A.nodes, most);
+  const int64_t pieces = kAdd ? 0 : ceil_div<int64_t>(A.nodes, fill.rows_of_piece);
+  if (A.n == 0) {
+    if (pieces > 0)
+      hipLaunchKernelGGL(k_fill, dim3(unsigned(pieces)), dim3(kBlock), 0, stream, fill);
+    return hipGetLastError();
   }
+  const EmbedPlan p = embed_plan(A.n, A.nodes, A.dim);
   char *const ws = static_cast<char *>(A.workspace);
+  Sums S{};
+  hipError_t e = sort(A, p, fill, pieces, stream, &S.pairs);
+  if (e != hipSuccess) return e;
   S.n = A.n;
   S.nodes = A.nodes;
   S.dim = A.dim;
@@ -534,16 +616,12 @@ hipError_t gradient(const hg_embed_grad_args &A, hipStream_t stream) {
   S.chunk = p.chunk;
   S.chunks = p.chunks;
   S.parts = reinterpret_cast<float *>(ws + p.parts);
-  S.marks = A.n > 0 ? reinterpret_cast<uint8_t *>(ws + p.marks) : nullptr;
+  S.ends = reinterpret_cast<int32_t *>(ws + p.ends);
   const int64_t vectors = ceil_div<int64_t>(A.dim, kVec<T>);
   int64_t lanes = 8;
   while (lanes < vectors && lanes < kBlock) lanes *= 2;
   S.slices = ceil_div<int64_t>(vectors, lanes);
-  S.sum_blocks = ceil_div<int64_t>(p.chunks, kBlock / lanes) * S.slices;
-  // a block fills some 64 KB
-  S.fill_rows = std::max<int64_t>(1, 65536 / (A.dim * int64_t(sizeof(O))));
-  S.blocks = S.sum_blocks + (kAdd ? 0 : ceil_div<int64_t>(A.nodes, S.fill_rows));
-  if (S.blocks == 0) return hipSuccess;
+  S.blocks = ceil_div<int64_t>(p.chunks, kBlock / lanes) * S.slices;
   const dim3 grid(unsigned(std::min(S.blocks, kMostBlocks))), block(kBlock);
   switch (lanes) {
     case 8: hipLaunchKernelGGL((k_embed_sum<T, O, kAdd, 8>), grid, block, 0, stream, S); break;
@@ -553,7 +631,7 @@ hipError_t gradient(const hg_embed_grad_args &A, hipStream_t stream) {
     case 128: hipLaunchKernelGGL((k_embed_sum<T, O, kAdd, 128>), grid, block, 0, stream, S); break;
     default: hipLaunchKernelGGL((k_embed_sum<T, O, kAdd, 256>), grid, block, 0, stream, S);
   }
-  const hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || p.chunks < 2) return e;
   const int64_t places = (p.chunks - 1) * ceil_div<int64_t>(A.dim, 128);
   hipLaunchKernelGGL((k_embed_join<O, kAdd>), dim3(unsigned(std::min(places, kMostBlocks))), block, 0,
@@ -578,8 +656,8 @@ hipError_t launch_embed(const hg_embed_args &A, hipStream_t stream) {
   }
 }
 
-int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim, bool add) {
-  return n > 0 ? embed_plan(n, nodes, dim, add).total : 0;
+int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim) {
+  return n > 0 ? embed_plan(n, nodes, dim).total : 0;
 }
 
 hipError_t launch_embed_grad(const hg_embed_grad_args &A, hipStream_t stream) {
