@@ -410,13 +410,14 @@ struct Columns {
 
 // The scales on the columns' sums v of R rows, i and every step-th after it.
 // (By mantissas and exponents for all, the 8-bit batch took 422 us, with the mild ones apart 416.)
+// by_row: the rows' scales, where they have been loaded.
 template <Scales kScales, int N, int R>
 __device__ __forceinline__ void scale(const Epilogue &E, const Columns<N> &C, int64_t i, int step,
-                                      float (&v)[R][N]) {
+                                      const float *by_row, float (&v)[R][N]) {
   if constexpr (kScales != Scales::kNone) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const float by = E.row_scale[min<int64_t>(i + r * step, E.rows - 1)];
+      const float by = by_row ? by_row[r] : E.row_scale[min<int64_t>(i + r * step, E.rows - 1)];
 #pragma unroll
       for (int k = 0; k < N; ++k)
         v[r][k] = kScales == Scales::kMild ? v[r][k] * (by * C.scale[k])
@@ -429,7 +430,8 @@ __device__ __forceinline__ void scale(const Epilogue &E, const Columns<N> &C, in
 // type); `residual`: the rows'.
 template <typename O, bool kPlain, Scales kScales, int N, int R>
 __device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, int64_t i, int step,
-                                       const Vec<O, N> *residual, float (&v)[R][N]) {
+                                       const Vec<O, N> *residual, float (&v)[R][N],
+                                       const float *by_row = nullptr) {
   const auto write = [&](void *to, int64_t stride) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -440,7 +442,7 @@ __device__ __forceinline__ void finish(const Epilogue &E, const Columns<N> &C, i
     write(E.y, E.y_stride);
     return;
   }
-  scale<kScales>(E, C, i, step, v);
+  scale<kScales>(E, C, i, step, by_row, v);
   if (E.bias) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -509,6 +511,8 @@ __device__ __forceinline__ void tile_of(const Product &A, int64_t b, int64_t &ti
 // themselves (the gradient of 4096 x 4096 weights over 8 rows: 36 us, now 20).  A lane keeps its columns; the residual
 // is loaded 16 rows ahead.
 // kPlain: nothing but the sums (the gradients).  kScaled: with scales, mild ones or not.
+// kDeep: how many times 16 rows of the residual are in flight.  Where the products take little time
+// (kDeep > 1) the scales of all rows are loaded first, too.
 template <int N, int NJ>
 struct Out {
   static constexpr int WJ = NJ * 16;
@@ -533,7 +537,7 @@ struct Out {
           *reinterpret_cast<const f32x4 *>(out + (u * kDown + r) * LD + c + h);
   }
 };
-template <bool kPlain, bool kScaled, int NI, int NJ>
+template <bool kPlain, bool kScaled, int kDeep, int NI, int NJ>
 __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i0, int64_t j0,
                                           const f32x4 (&acc)[NI][NJ], bool mild) {
   const Epilogue &E = A.E;
@@ -563,22 +567,32 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
     // 36 us, one row each 39)
     constexpr int R = L.U < 2 ? L.U : 2;
     const Columns<N> C(E, j0 + L.c);
-    Vec<O, N> res[L.U];
+    Vec<O, N> res[kDeep][L.U];
     const auto ahead = [&](int a) {
 #pragma unroll
       for (int u = 0; u < L.U; ++u) {
         const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
-        if (!kPlain && i < E.rows && C.n > 0) load_residual(E, C, i, res[u]);
+        if (!kPlain && i < E.rows && C.n > 0) load_residual(E, C, i, res[a % kDeep][u]);
       }
     };
-    ahead(0);
+    constexpr bool kByRow = kDeep > 1 && decltype(scales)::value != Scales::kNone;
+    float by[kByRow ? NI : 1][L.U];
+    if constexpr (kByRow) {
+#pragma unroll
+      for (int a = 0; a < NI; ++a)
+#pragma unroll
+        for (int u = 0; u < L.U; ++u)
+          by[a][u] = E.row_scale[min<int64_t>(i0 + 16 * a + u * L.kDown + L.r, E.rows - 1)];
+    }
+#pragma unroll
+    for (int a = 0; a < kDeep && a < NI; ++a) ahead(a);
 #pragma unroll
     for (int a = 0; a < NI; ++a) {
       L.exchange(acc[a]);
       Vec<O, N> now[L.U];
 #pragma unroll
       for (int u = 0; u < L.U; ++u) {
-        now[u] = res[u];
+        now[u] = res[a % kDeep][u];
         if (!kPlain) {  // (waited for here, not behind these rows' stores: 133 us, 138 without
                         // in 65537 x 512 x 1024 with residual and pre)
           u32x4 raw = __builtin_bit_cast(u32x4, now[u]);
@@ -586,7 +600,7 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
           now[u] = __builtin_bit_cast(Vec<O, N>, raw);
         }
       }
-      if (a + 1 < NI) ahead(a + 1);
+      if (a + kDeep < NI) ahead(a + kDeep);
 #pragma unroll
       for (int u = 0; u < L.U; u += R) {
         const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
@@ -594,7 +608,8 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
 #pragma unroll
         for (int t = 0; t < R; ++t) L.take(u + t, v[t]);
         if (i < E.rows && C.n > 0)
-          finish<O, kPlain, decltype(scales)::value>(E, C, i, L.kDown, now + u, v);
+          finish<O, kPlain, decltype(scales)::value>(E, C, i, L.kDown, now + u, v,
+                                                     kByRow ? by[a] + u : nullptr);
       }
       wave_sync();
     }
@@ -608,6 +623,11 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
       write(type, std::integral_constant<Scales, Scales::kAny>());
   });
 }
+
+// (In 256 x 256 tiles of integers it spills: 16384 x 4096 x 4096 289 us by 4, 259 by 1; 512 x 4096 x
+// 4096 17.8 and 20.1, 1001 x 2064 x 4099 22.2 and 23.7.)
+template <typename S, int BI>
+constexpr int kAheadOut = std::is_same_v<S, I8> && BI < 256 ? 4 : 1;
 
 // Whether all scales of a wavefront's part of C are mild.
 template <int NI, int NJ>
@@ -694,7 +714,7 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
   __syncthreads();
   bool mild = true;
   if constexpr (kScaled) mild = all_mild<NI, NJ>(A.E, i0 + wi, j0 + wj);
-  write_out<TP, kScaled>(A, lds, i0 + wi, j0 + wj, acc, mild);
+  write_out<TP, kScaled, kAheadOut<S, BI>>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
 
 // 16 bytes of zeros: where lanes past an operand's end load from.
@@ -849,6 +869,12 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
           mma_row(tp, St(&fq[a][h]), acc[a]);
         }
       }
+      // (of integers all fragments are read first, whose products take half as long as others': the
+      // batch of 16384 x 4096 x 4096 took 267 us as the compiler mixes them, 259 so)
+      if constexpr (std::is_same_v<S, I8>) {
+        __builtin_amdgcn_sched_group_barrier(0x100, kFrags * (NI + NJ), 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kFrags * NI * NJ, 0);
+      }
     }
   };
   multiply_all(acc, Step<std::conditional_t<kPlain32, Plain32, S>>());
@@ -879,7 +905,7 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
 #pragma unroll
     for (int b = 0; b < NJ; ++b) acc[a][b] = summed<S>(acc[a][b]);
   __syncthreads();
-  write_out<TP, kScaled>(A, lds, i0 + wi, j0 + wj, acc, mild);
+  write_out<TP, kScaled, kAheadOut<S, BI>>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
 
 // Adds the parts of a product in a fixed order, then the epilogue.  kShare threads share N
@@ -917,7 +943,7 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
       for (int k = 0; k < N; ++k) v[k] += red[s][at][k];
   }
   if (!in) return;
-  scale<kScales>(E, C, i, 0, sums);
+  scale<kScales>(E, C, i, 0, nullptr, sums);
   with_type(E.dtype, [&](auto type) {
     Vec<decltype(type), N> r;
     load_residual(E, C, i, r);
@@ -1134,20 +1160,30 @@ __global__ __launch_bounds__(256) void k_dz(const T *dy, int64_t dy_stride, Pre 
 // ---- operands laid out anew ---------------------------------------------------------
 
 // Rows of `cols` elements into rows of per_row 16-byte pieces, the last one's rest zeros.
+struct Lay {
+  const void *from;
+  int64_t stride, cols;
+  uint32_t per_row, pieces;
+  u32x4 *to;
+};
+// Two operands by one launch (a launch of its own took each some 8 us, of 42 for 1001 x 2050 x 4099 in
+// 8-bit integers): the first `blocks` blocks take A.
 template <typename S>
-__global__ __launch_bounds__(256) void k_lay(const S *from, int64_t stride, int64_t cols,
-                                             uint32_t per_row, uint32_t pieces, u32x4 *to) {
+__global__ __launch_bounds__(256) void k_lay(Lay A, Lay B, uint32_t blocks) {
+  const bool first = blockIdx.x < blocks;
+  const Lay &L = first ? A : B;
+  const uint32_t b = first ? blockIdx.x : blockIdx.x - blocks;
   u32x4 v[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    const uint32_t t = blockIdx.x * 1024 + u * 256 + threadIdx.x;
-    const int64_t row = t / per_row, c = int64_t(t % per_row) * (16 / int(sizeof(S)));
-    if (t < pieces) v[u] = row_piece(from + row * stride, c, cols);
+    const uint32_t t = b * 1024 + u * 256 + threadIdx.x;
+    const int64_t row = t / L.per_row, c = int64_t(t % L.per_row) * (16 / int(sizeof(S)));
+    if (t < L.pieces) v[u] = row_piece(static_cast<const S *>(L.from) + row * L.stride, c, L.cols);
   }
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    const uint32_t t = blockIdx.x * 1024 + u * 256 + threadIdx.x;
-    if (t < pieces) to[t] = v[u];
+    const uint32_t t = b * 1024 + u * 256 + threadIdx.x;
+    if (t < L.pieces) L.to[t] = v[u];
   }
 }
 
@@ -1162,17 +1198,26 @@ bool is_direct(const Operand &O, bool turned, int64_t depth) {
          (O.padded || (turned ? O.rows : depth) % E == 0);
 }
 
-// Copies an operand of rows x cols to `to`.
+// The copy of an operand of rows x cols to `to`, which takes its place.
 template <typename S>
-hipError_t lay(Operand &O, int64_t rows, int64_t cols, bool turned, char *to, hipStream_t stream) {
+Lay lay_of(Operand &O, int64_t rows, int64_t cols, bool turned, char *to) {
   const int64_t stride = padded(cols, sizeof(S));
   const uint32_t per_row = uint32_t(stride * sizeof(S) / 16);
-  const int64_t n = rows * per_row;  // (below 2^30)
-  hipLaunchKernelGGL((k_lay<S>), dim3(unsigned(ceil_div<int64_t>(n, 1024))), dim3(256), 0, stream,
-                     static_cast<const S *>(O.p), O.stride, cols, per_row, uint32_t(n),
-                     reinterpret_cast<u32x4 *>(to));
+  const Lay l{O.p, O.stride, cols, per_row, uint32_t(rows * per_row),  // (below 2^30)
+              reinterpret_cast<u32x4 *>(to)};
   O = Operand{to, stride, turned ? stride : rows, true};
+  return l;
+}
+template <typename S>
+hipError_t lay(const Lay &A, const Lay &B, hipStream_t stream) {
+  const uint32_t a = ceil_div<uint32_t>(A.pieces, 1024), b = ceil_div<uint32_t>(B.pieces, 1024);
+  hipLaunchKernelGGL((k_lay<S>), dim3(a + b), dim3(256), 0, stream, A, B, a);
   return hipGetLastError();
+}
+template <typename S>
+hipError_t lay(Operand &O, int64_t rows, int64_t cols, bool turned, char *to, hipStream_t stream) {
+  const Lay l = lay_of<S>(O, rows, cols, turned, to);
+  return lay<S>(l, Lay{l.from, 0, 0, 1, 0, nullptr}, stream);
 }
 
 template <typename S, bool TP, bool TQ, int BI, int BJ, int kWavesI, int kWavesJ, int W,
@@ -1331,8 +1376,9 @@ hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
   const LinearSpace s = linear_space(A.m, A.k, A.n, A.dtype);
   char *const ws = static_cast<char *>(A.workspace);
   if (s.laid) {
-    hipError_t e = lay<T>(w, A.n, A.k, false, ws + s.w, stream);
-    if (e == hipSuccess) e = lay<T>(x, A.m, A.k, false, ws + s.x, stream);
+    const Lay lw = lay_of<T>(w, A.n, A.k, false, ws + s.w);
+    const Lay lx = lay_of<T>(x, A.m, A.k, false, ws + s.x);
+    const hipError_t e = lay<T>(lw, lx, stream);
     if (e != hipSuccess) return e;
   }
   return product<T, false, false>(w, x, A.k, E, reinterpret_cast<float *>(ws + s.parts), stream);
