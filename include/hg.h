@@ -49,8 +49,8 @@ typedef enum hg_status {
 
 /* Element type of a feature table.  The gather copies bytes; the type only
  * fixes the element size (4, 2, 2 bytes).  HG_DT_E4M3 (8 bits: 4 of exponent,
- * 3 of mantissa, no infinities, largest value 448) is a type of the dense
- * operators only, not of feature tables. */
+ * 3 of mantissa, no infinities, largest value 448) and HG_DT_I8 (8-bit
+ * integers) are types of the dense operators only, not of feature tables. */
 typedef enum hg_dtype {
   HG_DT_NONE = 0,
   HG_DT_F32 = 1,
@@ -580,8 +580,8 @@ hg_status hg_bench_philox(uint64_t rng_seed, int32_t hop, int32_t etype, int64_t
  *  - Arrays are device memory on the current device, borrowed until the work
  *    on `stream` is done.  Every call is asynchronous, allocates nothing and
  *    waits for nothing, so it can be captured in a graph.
- *  - Types: float32, float16 and bfloat16 (`dtype`), and 8 bits (HG_DT_E4M3)
- *    where a call says so.  Sums, statistics and everything between the reads
+ *  - Types: float32, float16 and bfloat16 (`dtype`), and 8 bits (HG_DT_E4M3,
+ *    and integers, HG_DT_I8) where a call says so.  Sums, statistics and everything between the reads
  *    and the result are held in 32 bits; a result is rounded once, to nearest
  *    even, unless a call says otherwise.
  *  - A result does not depend on timing: no sum is made by atomics.
@@ -662,7 +662,7 @@ int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim);
  * sum (NULL: not written) receives h in `dtype`; the norm is of the unrounded h.
  * y in `dtype`; or in 8 bits with a scale per row, so that y8_j scale_i stands for y_j:
  *   out_dtype HG_DT_E4M3   scale_i = max(max_j |y_j| / 448, 2^-126),  y8_j = e4m3(y_j / scale_i)
- *   out_dtype HG_DT_I8     scale_i = max(max_j |y_j| / 127, 2^-126),  y8_j = y_j / scale_i,
+ *   out_dtype HG_DT_I8     scale_i = max(max_j |y_j| (1 / 127), 2^-126),  y8_j = y_j / scale_i,
  *                          rounded to the nearest integer (of two as near, the even one)
  * The mean is taken first and the squares are summed around it, in float32.  A NaN or an infinity
  * anywhere in a row, or a sum past float32's range, makes its y NaN (and its scale); in 8-bit
@@ -763,9 +763,9 @@ int64_t hg_embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim);
 /* Rows in 8-bit integers, for products of integers or to keep activations in half the memory or
  * less until the backward pass.  Over each row (group 0), or over each HG_KEPT_GROUP columns of a row
  * (group HG_KEPT_GROUP; the last group may be shorter):
- *   scale = max(max_j |x_j| / 127, 2^-126),  q_j = x_j / scale
- * in float32, rounded to the nearest integer (of two as near, the even one), so that q_j scale
- * stands for x_j, within half a scale of it.  A row (or group) with a NaN or an infinity is zeros with a
+ *   scale = max(max_j |x_j| (1 / 127), 2^-126),  q_j = x_j / scale
+ * in float32 (1 / 127, the product, the quotient), rounded to the nearest integer (of two as near,
+ * the even one), so that q_j scale stands for x_j, within half a scale of it.  A row (or group) with a NaN or an infinity is zeros with a
  * scale of NaN. */
 #define HG_KEPT_GROUP 128
 typedef struct hg_quantize_args {

@@ -253,7 +253,7 @@ hg_status hg_dequantize(const hg_dequantize_args *a, hipStream_t stream) {
              "hg_dequantize: x is NULL or its stride below dim");
   clear_pending();
   return launched(launch_dequantize(kept(a->q, a->q_stride, a->scale, a->group, a->dim), a->rows,
-                                    a->dim, a->dim, a->dtype, a->x, a->x_stride, stream),
+                                    a->dim, a->dim, a->dtype, a->x, a->x_stride, false, stream),
                   "hg_dequantize");
 }
 

@@ -36,9 +36,10 @@ int64_t embed_grad_workspace(int64_t n, int64_t nodes, int64_t dim);
 
 struct Kept;
 hipError_t launch_quantize(const hg_quantize_args &A, hipStream_t stream);
-// Rows of `cols` values, and zeros from there to out_cols.
+// Rows of `cols` values, and zeros from there to out_cols; read_next: by what follows on the stream.
 hipError_t launch_dequantize(const Kept &K, int64_t rows, int64_t cols, int64_t out_cols,
-                             int32_t dtype, void *out, int64_t stride, hipStream_t stream);
+                             int32_t dtype, void *out, int64_t stride, bool read_next,
+                             hipStream_t stream);
 
 hipError_t launch_linear(const hg_linear_args &A, hipStream_t stream);
 int64_t linear_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype);

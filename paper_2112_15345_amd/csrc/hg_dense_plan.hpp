@@ -257,9 +257,12 @@ inline EmbedPlan embed_plan(int64_t n, int64_t nodes, int64_t dim) {
   p.passes = (p.bits + most - 1) / most;
   p.digit = (p.bits + p.passes - 1) / p.passes;
   p.tiles = ceil_div<int64_t>(n, kSortTile);
-  // chunks that fill the units, as long as they can be for that: each leaves up to two parts
+  // chunks that fill the units, as long as they can be for that: each leaves up to two parts (us,
+  // 65537 words of 1024 columns by chunks of 16 / 32 / 64 / 128: 126 / 115 / 110 / 115; 175514 words
+  // of 25, 16 columns, by 8: 138, the parts' sums nearly all of it)
   p.chunk = 8;
-  while (p.chunk < 64 && n * std::min<int64_t>(dim, 2048) > (p.chunk << 21)) p.chunk *= 2;
+  while (p.chunk < 64 && (n * std::min<int64_t>(dim, 2048) > (p.chunk << 21) || n > (p.chunk << 13)))
+    p.chunk *= 2;
   p.chunks = ceil_div<int64_t>(n, p.chunk);
   const int64_t bins = int64_t(1) << p.digit;
   p.pairs = 0;

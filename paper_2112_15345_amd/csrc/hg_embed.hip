@@ -125,25 +125,35 @@ struct Fill {
   void *out;
   int64_t stride, rows, dim;
   int32_t size;  // bytes of an element
-  int64_t rows_of_piece, first, own;
+  int64_t rows_of_piece;  // 0: the rows follow each other without gaps, and are filled as one
+  int64_t first, own;
 };
+constexpr int64_t kFillBytes = 65536;
+__device__ __forceinline__ void fill_bytes(void *at, int n) {
+  Vec<uint8_t, 16> none;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) none.e[k] = 0;
+  none.template store<Move::kStreamed>(static_cast<uint8_t *>(at), n);
+}
 // Whether this block fills.
 __device__ __forceinline__ bool filled(const Fill &F) {
   if (int64_t(blockIdx.x) < F.own) return false;
-  const int64_t r0 = (F.first + blockIdx.x - F.own) * F.rows_of_piece;
+  const int64_t piece = F.first + blockIdx.x - F.own;
+  uint8_t *const out = static_cast<uint8_t *>(F.out);
+  if (F.rows_of_piece == 0) {
+    const int64_t bytes = F.rows * F.dim * F.size, end = min(bytes, (piece + 1) * kFillBytes);
+    for (int64_t c = piece * kFillBytes + threadIdx.x * 16; c < end; c += blockDim.x * 16)
+      fill_bytes(out + c, int(min<int64_t>(16, bytes - c)));
+    return true;
+  }
+  const int64_t r0 = piece * F.rows_of_piece, bytes = F.dim * F.size;
   const uint32_t rows = uint32_t(min(F.rows_of_piece, F.rows - r0));
-  const int64_t bytes = F.dim * F.size;
   const uint32_t across = uint32_t((bytes + 15) / 16);
   for (uint64_t t = threadIdx.x; t < uint64_t(rows) * across; t += blockDim.x) {
-    const uint32_t r = uint32_t(t) / across;  // (either there is one row, or t is small)
-    const int64_t row = rows == 1 ? 0 : r;
+    // (either there is one row, or few enough pieces of 16 bytes for 32 bits)
+    const int64_t row = rows == 1 ? 0 : uint32_t(t) / across;
     const int64_t c = (int64_t(t) - row * across) * 16;
-    Vec<uint8_t, 16> none;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) none.e[k] = 0;
-    none.template store<Move::kStreamed>(
-        static_cast<uint8_t *>(F.out) + (r0 + row) * F.stride * F.size + c,
-        int(min<int64_t>(16, bytes - c)));
+    fill_bytes(out + (r0 + row) * F.stride * F.size + c, int(min<int64_t>(16, bytes - c)));
   }
   return true;
 }
@@ -487,7 +497,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(Sums A, int64_t places) {
     float s[N] = {};
     if (n > 0) {
       // part 0 is the chunk's own, the others came into their chunks
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t k = turn; k <= last - chunk; k += kDown) {
         Vec<float, N> t;
         t.load(A.parts + (2 * (chunk + k) + (k == 0)) * A.dim + c, n);
@@ -589,12 +599,19 @@ __global__ __launch_bounds__(kBlock) void k_fill(Fill fill) { filled(fill); }
 template <typename T, typename O, bool kAdd>
 hipError_t gradient(const hg_embed_grad_args &A, hipStream_t stream) {
   Fill fill{A.dtable, A.dtable_stride, A.nodes, A.dim, int32_t(sizeof(O)), 0, 0, 0};
-  fill.rows_of_piece = std::max<int64_t>(1, 65536 / (A.dim * int64_t(sizeof(O))));
-  // (a launch has fewer than 2^32 threads, of 1024 in a block)
-  const int64_t most = int64_t(1) << 21;
-  if (ceil_div<int64_t>(A.nodes, fill.rows_of_piece) > most)
-    fill.rows_of_piece = ceil_div<int64_t>(A.nodes, most);
-  const int64_t pieces = kAdd ? 0 : ceil_div<int64_t>(A.nodes, fill.rows_of_piece);
+  int64_t pieces = 0;
+  if (!kAdd) {
+    const int64_t row = A.dim * int64_t(sizeof(O));
+    // (a launch has fewer than 2^32 threads, of 1024 in a block; as one, 2^21 pieces are 128 GB)
+    const int64_t most = int64_t(1) << 21;
+    if ((A.nodes == 1 || A.dtable_stride == A.dim) && A.nodes <= most * kFillBytes / row) {
+      pieces = ceil_div<int64_t>(A.nodes * row, kFillBytes);
+    } else {
+      fill.rows_of_piece =
+          std::max(ceil_div<int64_t>(A.nodes, most), std::max<int64_t>(1, kFillBytes / row));
+      pieces = ceil_div<int64_t>(A.nodes, fill.rows_of_piece);
+    }
+  }
   if (A.n == 0) {
     if (pieces > 0)
       hipLaunchKernelGGL(k_fill, dim3(unsigned(pieces)), dim3(kBlock), 0, stream, fill);

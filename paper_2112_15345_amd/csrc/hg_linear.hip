@@ -1445,7 +1445,7 @@ hipError_t linear_grad(const hg_linear_grad_args &A, const Kept &kept_x, const K
       // what the rows stand for, in T (the products' instructions take it): a rounding more than
       // the integers and their scales have, of 2^-9 at most where their own step is some 2^-8
       const int64_t stride = padded(A.k, sizeof(T));
-      e = launch_dequantize(kept_x, A.m, A.k, stride, A.dtype, ws + g.x, stride, stream);
+      e = launch_dequantize(kept_x, A.m, A.k, stride, A.dtype, ws + g.x, stride, true, stream);
       x = Operand{ws + g.x, stride, stride, true};
     } else if (g.laid) {
       e = lay<T>(x, A.m, A.k, true, ws + g.x, stream);

@@ -68,7 +68,7 @@ template <bool kIntegers = false>
 __device__ __forceinline__ float scale_of(uint32_t amax) {
   const float a = __uint_as_float(amax);
   // (not fmax: it would drop a NaN)
-  const float c = a / (kIntegers ? 127.0f : 448.0f);
+  const float c = kIntegers ? a * (1.0f / 127.0f) : a / 448.0f;
   if (kIntegers && !(c < INFINITY)) return __builtin_nanf("");
   return c < 0x1p-126f ? 0x1p-126f : c;
 }

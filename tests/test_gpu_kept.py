@@ -1,5 +1,5 @@
 """quantize, dequantize, and linear_grad from kept rows.  The integers are the definition's bit for bit:
-in float32, by division, on the CPU."""
+in float32, the quotients by division, on the CPU."""
 import math
 
 import numpy as np
@@ -27,7 +27,8 @@ def define(x, group):
     for g in range(scale.shape[1]):
         part = x[:, g * width:(g + 1) * width]
         top = np.abs(part).max(1)
-        c = np.maximum(top / np.float32(127), np.float32(2.0 ** -126)).astype(np.float32)
+        c = top * (np.float32(1) / np.float32(127))
+        c = np.maximum(c, np.float32(2.0 ** -126)).astype(np.float32)
         c[~np.isfinite(top)] = np.nan
         fine = np.isfinite(c)
         q[fine, g * width:(g + 1) * width] = np.rint(part[fine] / c[fine, None]).astype(np.int8)
@@ -57,7 +58,10 @@ def test_quantize(dim, dtype, group):
         for out in (F32, F16, BF16):
             back = hg.dequantize(*got, group=group, out_dtype=out)
             c = got[1].repeat_interleave(GROUP, 1)[:, :dim] if group else got[1][:, None]
-            assert torch.equal(back, (got[0].float() * c).to(out))
+            # one rounding to the type, or one to float32 before it
+            want = got[0].double() * c.double()
+            assert back.dtype == out
+            R.assert_close(back, want, R.rounding(want, out) + R.E * want.abs(), "back")
 
 
 def test_many_rows():
@@ -74,7 +78,7 @@ def test_middles(dtype):
         check((step * scale)[None].to(dtype), 0, hg.quantize((step * scale)[None].to(dtype)))
     # scales that are no powers of two, elements as near to the middles as float32 has them
     for top in (1.0, 3.7, 100.1, 5e-30, 1e30):
-        c = torch.tensor(top, dtype=F32) / 127
+        c = torch.tensor(top, dtype=F32) * (torch.ones(()) / 127)
         mid = (torch.arange(-126, 126, dtype=F32) + 0.5) * c
         row = torch.cat([torch.tensor([top]), mid, torch.nextafter(mid, mid + 1e38),
                          torch.nextafter(mid, mid - 1e38)])[None].cuda()
