@@ -19,7 +19,8 @@ constexpr int kBlock = 256;
 // ---- forward -------------------------------------------------------------------
 
 // 16 bytes of the result a lane; `across` lanes share a row (as many as it has vectors, or the
-// block), and a lane has kAhead rows in flight.
+// block), and a lane has kAhead rows in flight.  65537 words of 1024 columns, float32 to bfloat16: 40 us, 4.9
+// TB/s; with 16 bytes of the row a lane, 8 of the result, 42.
 template <typename T, typename O>
 __global__ __launch_bounds__(kBlock) void k_embed(hg_embed_args A, int32_t across) {
   constexpr int V = kVec<O>, kAhead = 4;

@@ -42,6 +42,9 @@ def some_ids(n, nodes, kind, seed=0):
 def sums(dy, ids, nodes):
     ok = (ids >= 0) & (ids < nodes)
     d = torch.zeros(nodes, dy.shape[1], dtype=torch.float64, device="cuda")
+    if len(ids) and bool((ids == ids[0]).all()) and bool(ok[0]):  # (the additions below would queue)
+        d[ids[0]] = dy.double().sum(0)
+        return d
     return d.index_add_(0, ids[ok], dy[ok].double())
 
 
