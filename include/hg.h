@@ -665,10 +665,12 @@ int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim);
  *   out_dtype HG_DT_I8     scale_i = max(max_j |y_j| (1 / 127), 2^-126),  y8_j = y_j / scale_i,
  *                          rounded to the nearest integer (of two as near, the even one)
  * The mean is taken first and the squares are summed around it, in float32.  A NaN or an infinity
- * anywhere in a row, or a sum past float32's range, makes its y NaN (and its scale); in 8-bit
- * integers, which have no NaN, the row is zeros and its scale NaN.  An id outside [0, x_rows) makes
- * the row such a row: nothing is read for it and nothing waits to report it.  With eps 0 a row
- * of equal elements has no y: it is NaN, or what rounding makes of it.
+ * anywhere in a row, or a sum (of h or of d_j^2, elements of some 1e19) past float32's range, makes
+ * its y NaN (and its scale); in 8-bit integers, which have no NaN, the row is zeros and its scale
+ * NaN.  An id outside [0, x_rows) makes the row such a row: nothing is read for it and nothing waits
+ * to report it.  With eps 0 a row of equal elements has no y: it is NaN, or what rounding makes of
+ * it; and squares below float32's range (d of some 1e-20) are lost or inexact, which an eps above
+ * 1e-37 hides.
  * sum may be x (without ids) or residual, y may be x (without ids) or residual (in `dtype`),
  * each with the same stride. */
 typedef struct hg_layer_norm_args {
@@ -696,6 +698,7 @@ hg_status hg_layer_norm(const hg_layer_norm_args *args, hipStream_t stream);
  * dsum of sum (NULL: none):
  *   g = dy weight,  n = d s,  dx = s (g - mean(g) - n mean(g n)) + dsum,
  *   dweight_j = sum_i dy_ij n_ij,  dbias_j = sum_i dy_ij
+ * A row that breaks as above has a dx of NaN, and makes dweight NaN.
  * dx is the gradient of both x and residual (row i belongs to x[ids[i]]); dx, dweight and dbias may
  * each be NULL (not computed).  An 8-bit y counts as unrounded.  dx may be dy or dsum or (without
  * ids) x, with the same stride.  dweight and dbias are summed over the rows in a fixed order. */

@@ -34,6 +34,13 @@ hipError_t by_rows(int64_t rows, int64_t vecs, int64_t few, F f) {
   return f.template run<256, 0>();
 }
 
+// 1 / sqrt(var + eps), of ss squares around the mean: NaN where they pass float32's range, as the
+// header has it (0 there would leave the bias as the row's values).
+__device__ __forceinline__ float inverse_deviation(float ss, float count, float eps) {
+  const float v = ss / count + eps;
+  return v < INFINITY ? rsqrtf(v) : __builtin_nanf("");
+}
+
 // Where 8-bit results go, and how: kOut is HG_DT_NONE (x's type), HG_DT_E4M3 or HG_DT_I8.
 template <int kOut, int V>
 __device__ __forceinline__ void store_8(uint8_t *p, const float *v, int n) {
@@ -133,7 +140,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm(hg_layer_norm_args A) {
         ss += h[v][j] * h[v][j];
       }
     }
-    const float s = rsqrtf(grp.sum(ss) / count + A.eps);
+    const float s = inverse_deviation(grp.sum(ss), count, A.eps);
     uint32_t amax = 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -202,7 +209,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_long(hg_layer_norm_args A
         ss += d * d;
       }
     }
-    const float s = rsqrtf(grp.sum(ss) / count + A.eps);
+    const float s = inverse_deviation(grp.sum(ss), count, A.eps);
     auto value = [&](uint32_t c, const float *h, float *y) {
       float w[V], b[V];
       load_columns<T>(A.weight, A.weight_dtype, 1.0f, c, dim - c, w);
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_grad(hg_layer_norm_grad_a
       }
     }
     grp.sum(ss, gd);
-    const float s = rsqrtf(ss / count + A.eps);
+    const float s = inverse_deviation(ss, count, A.eps);
     const float k = gd / count * s * s;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -439,7 +446,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_grad_long(hg_layer_norm_g
       }
     }
     grp.sum(ss, gd);
-    const float s = rsqrtf(ss / count + A.eps);
+    const float s = inverse_deviation(ss, count, A.eps);
     const float k = gd / count * s * s;
     for (uint32_t c = threadIdx.x * V; c < dim; c += kBlock * V) {
       const int n = dim - c;

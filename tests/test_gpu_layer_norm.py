@@ -297,3 +297,38 @@ def test_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("dtype,dim", [(F32, 64), (F32, 1000), (F32, 9000), (BF16, 40), (BF16, 2048),
+                                       (BF16, 20_001)])
+def test_squares_past_the_range(dtype, dim):
+    """A finite row whose squares (or their sum) pass float32's range is NaN, whatever the bias and the
+    result's type, and so is what its gradient reaches; the other rows are as they are by themselves."""
+    x, r, dy = (rand(7, dim, dtype=dtype, seed=s) for s in (1, 2, 3))
+    x[1] = 1e20
+    x[1, ::2] = -1e20
+    x[2] *= 3e19
+    x[4, dim // 3] = 2e19  # (one square alone)
+    x[6] *= 1e15           # (squares that stay in it)
+    bad, good = [1, 2, 4], [0, 3, 5, 6]
+    w, b = 1 + rand(dim, seed=4, scale=0.1), rand(dim, seed=5)
+    for residual in (None, r):
+        part = None if residual is None else r[good]
+        for out in (dtype, E4M3, I8):
+            y, total, scale = hg.layer_norm(x, w, b, residual=residual, out_dtype=out)
+            want = hg.layer_norm(x[good], w, b, residual=part, out_dtype=out)
+            check_forward(x[good], w, b, part, 1e-5, out, want)
+            assert torch.equal(y[good].float(), want[0].float())
+            if out == I8:
+                assert not y[bad].any()
+            else:
+                assert torch.isnan(y[bad].float()).all()
+            if out != dtype:
+                assert torch.isnan(scale[bad]).all() and torch.equal(scale[good], want[2])
+            if residual is not None:
+                assert torch.isfinite(total.float()).all()
+    for ds in (None, r):
+        dx, dw, db = hg.layer_norm_grad(dy, x, w, dsum=ds)
+        want = hg.layer_norm_grad(dy[good], x[good], w, dsum=None if ds is None else ds[good])
+        assert torch.isnan(dx[bad].float()).all() and torch.equal(dx[good], want[0])
+        assert torch.isnan(dw).all() and torch.isfinite(db).all()
