@@ -804,8 +804,7 @@ hg_status hg_dequantize(const hg_dequantize_args *args, hipStream_t stream);
  *   z_ij = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,
  * and y, pre and residual in out_dtype (float32, float16 or bfloat16).
  * HG_DT_I8 is the same with 8-bit integers (-128 .. 127), whose sum over k is exact (k up to 131071,
- * HG_EUNSUPPORTED past it; rounded to float32 once, or once in each part of a product whose k is
- * cut).
+ * HG_EUNSUPPORTED past it) and rounded to float32 once, whatever m and n.
  * float32 products are made of 16-bit pieces that add up to the elements (of
  * elements below 2^-108 in size the pieces may lose the lower bits), and are
  * as exact as products in 32 bits; results that are not finite that way, as

@@ -31,7 +31,8 @@ struct F8 {
   uint8_t b;
 };
 // An element of 8-bit integers, whose products are summed exactly in 32-bit integers (of at most
-// 131071 terms of up to 2^14).  The sums stay in the registers of float32 ones until they are whole.
+// 131071 terms of up to 2^14).  The sums stay in the registers (and the parts of a depth that is cut in
+// the places) of float32 ones until they are whole, and are rounded to float32 once.
 // 16384 x 4096 x 4096 with bias and residual: 258 us, 2.13e15 operations a second (2.6e15 at a depth of
 // 8192 without residual; the library's product of integers alone 281 us).
 struct I8 {
@@ -92,14 +93,19 @@ __device__ __forceinline__ f32x4 mma(f32x4 c, u32x4 p, u32x4 q, I8) {
                                                    __builtin_bit_cast(i32x4, q),
                                                    __builtin_bit_cast(i32x4, c), 0, 0, 0));
 }
-// Whole sums as float32 values.
+// Whether sums are integers, held as the bits of float32 values.
 template <typename S>
-__device__ __forceinline__ f32x4 summed(f32x4 c) {
-  if constexpr (std::is_same_v<S, I8>) {
+constexpr bool kWhole = std::is_same_v<S, I8>;
+// N such sums as float32 values.
+template <int N>
+__device__ __forceinline__ void rounded(float *v) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = float(__float_as_int(c[e]));
-  }
-  return c;
+  for (int k = 0; k < N; ++k) v[k] = float(__float_as_int(v[k]));
+}
+// The sum of two sums.
+template <bool kInt>
+__device__ __forceinline__ float added(float a, float b) {
+  return kInt ? __int_as_float(__float_as_int(a) + __float_as_int(b)) : a + b;
 }
 
 struct Plain32 {};
@@ -311,7 +317,7 @@ struct Epilogue {
   void *pre;
   int64_t pre_stride;
   const float *row_scale, *col_scale;
-  float *part;  // [splits, rows, cols] sums to be joined, instead of the rest
+  float *part;  // [splits, rows, cols] sums to be joined (of integers their bits), instead of the rest
 };
 
 // (a reciprocal within 1 unit of 2^-23, where a division would cost as much as the rest)
@@ -513,7 +519,7 @@ __device__ __forceinline__ void tile_of(const Product &A, int64_t b, int64_t &ti
 // themselves (the gradient of 4096 x 4096 weights over 8 rows: 36 us, now 20).  A lane keeps its columns; the residual
 // is loaded 16 rows ahead.
 // kPlain: nothing but the sums (the gradients).  kScaled: with scales, mild ones or not.
-// kDeep: how many times 16 rows of the residual are in flight.  Where the products take little time
+// kInt: the sums are integers.  kDeep: how many times 16 rows of the residual are in flight.  Where the products take little time
 // (kDeep > 1) the scales of all rows are loaded first, too.
 template <int N, int NJ>
 struct Out {
@@ -539,7 +545,7 @@ struct Out {
           *reinterpret_cast<const f32x4 *>(out + (u * kDown + r) * LD + c + h);
   }
 };
-template <bool kPlain, bool kScaled, int kDeep, int NI, int NJ>
+template <bool kPlain, bool kScaled, bool kInt, int kDeep, int NI, int NJ>
 __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i0, int64_t j0,
                                           const f32x4 (&acc)[NI][NJ], bool mild) {
   const Epilogue &E = A.E;
@@ -608,7 +614,10 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
         const int64_t i = i0 + 16 * a + u * L.kDown + L.r;
         float v[R][N];
 #pragma unroll
-        for (int t = 0; t < R; ++t) L.take(u + t, v[t]);
+        for (int t = 0; t < R; ++t) {
+          L.take(u + t, v[t]);
+          if constexpr (kInt) rounded<N>(v[t]);
+        }
         if (i < E.rows && C.n > 0)
           finish<O, kPlain, decltype(scales)::value>(E, C, i, L.kDown, now + u, v,
                                                      kByRow ? by[a] + u : nullptr);
@@ -629,7 +638,7 @@ __device__ __forceinline__ void write_out(const Product &A, char *lds, int64_t i
 // (In 256 x 256 tiles of integers it spills: 16384 x 4096 x 4096 289 us by 4, 259 by 1; 512 x 4096 x
 // 4096 17.8 and 20.1, 1001 x 2064 x 4099 22.2 and 23.7.)
 template <typename S, int BI>
-constexpr int kAheadOut = std::is_same_v<S, I8> && BI < 256 ? 4 : 1;
+constexpr int kAheadOut = kWhole<S> && BI < 256 ? 4 : 1;
 
 // Whether all scales of a wavefront's part of C are mild.
 template <int NI, int NJ>
@@ -709,14 +718,10 @@ __global__ __launch_bounds__(256) void k_product(Product A) {
 #pragma unroll
         for (int b = 0; b < NJ; ++b) acc[a][b] = mma(acc[a][b], fp[b][h], fq[a][h], T());
   }
-#pragma unroll
-  for (int a = 0; a < NI; ++a)
-#pragma unroll
-    for (int b = 0; b < NJ; ++b) acc[a][b] = summed<S>(acc[a][b]);
   __syncthreads();
   bool mild = true;
   if constexpr (kScaled) mild = all_mild<NI, NJ>(A.E, i0 + wi, j0 + wj);
-  write_out<TP, kScaled, kAheadOut<S, BI>>(A, lds, i0 + wi, j0 + wj, acc, mild);
+  write_out<TP, kScaled, kWhole<S>, kAheadOut<S, BI>>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
 
 // 16 bytes of zeros: where lanes past an operand's end load from.
@@ -902,17 +907,14 @@ __global__ __launch_bounds__(64 * kWavesI *kWavesJ,
             acc[a][b][e] = finite(acc[a][b][e]) ? acc[a][b][e] : again[a][b][e];
     }
   }
-#pragma unroll
-  for (int a = 0; a < NI; ++a)
-#pragma unroll
-    for (int b = 0; b < NJ; ++b) acc[a][b] = summed<S>(acc[a][b]);
   __syncthreads();
-  write_out<TP, kScaled, kAheadOut<S, BI>>(A, lds, i0 + wi, j0 + wj, acc, mild);
+  write_out<TP, kScaled, kWhole<S>, kAheadOut<S, BI>>(A, lds, i0 + wi, j0 + wj, acc, mild);
 }
 
 // Adds the parts of a product in a fixed order, then the epilogue.  kShare threads share N
 // neighbours of a row (16 bytes of it): each adds every kShare-th part, the first adds theirs.
-template <int kShare, int N, Scales kScales>
+// kInt: the parts are integers, whose sum is exact, too.
+template <int kShare, int N, Scales kScales, bool kInt>
 __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
   constexpr int kAt = 256 / kShare;
   __shared__ float red[kShare > 1 ? kShare : 1][kShare > 1 ? kAt : 1][N + 1];
@@ -933,7 +935,7 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
     float a[N];
     get<float, N>(part, (s * E.rows + i) * E.cols + j, a, C.n);
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += a[k];
+    for (int k = 0; k < N; ++k) v[k] = added<kInt>(v[k], a[k]);
   }
   if constexpr (kShare > 1) {
 #pragma unroll
@@ -942,9 +944,10 @@ __global__ __launch_bounds__(256) void k_join(Epilogue E, int32_t splits) {
     if (share) return;
     for (int s = 1; s < kShare; ++s)
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] += red[s][at][k];
+      for (int k = 0; k < N; ++k) v[k] = added<kInt>(v[k], red[s][at][k]);
   }
   if (!in) return;
+  if constexpr (kInt) rounded<N>(v);
   scale<kScales>(E, C, i, 0, nullptr, sums);
   with_type(E.dtype, [&](auto type) {
     Vec<decltype(type), N> r;
@@ -1040,23 +1043,15 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Product A) {
   if (C.n <= 0) return;
   float sums[1][8] = {};
   float *const v = sums[0];
-  if constexpr (std::is_same_v<S, I8>) {
-    int32_t whole[8] = {};
-    for (int s = 0; s < kWaves; ++s)
+  for (int s = 0; s < kWaves; ++s)
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        whole[k] += __float_as_int(red[s][i >> 4][i & 15][(t & 1) * 8 + k]);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = float(whole[k]);
-  } else {
-    for (int s = 0; s < kWaves; ++s)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += red[s][i >> 4][i & 15][(t & 1) * 8 + k];
-  }
+    for (int k = 0; k < 8; ++k)
+      v[k] = added<kWhole<S>>(v[k], red[s][i >> 4][i & 15][(t & 1) * 8 + k]);
   if (A.E.part) {
     put<float, 8>(A.E.part, (int64_t(blockIdx.y) * A.E.rows + i) * A.E.cols + C.j, v, C.n);
     return;
   }
+  if constexpr (kWhole<S>) rounded<8>(v);
   if constexpr (kIs8<S>) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = scales[k].times(v[k]);
@@ -1238,24 +1233,23 @@ void launch_few(const Product &A, const FewPlan &p, hipStream_t stream) {
     hipLaunchKernelGGL((k_few<S, G, 16>), grid, dim3(1024), 0, stream, A);
 }
 
-template <int N, Scales kScales>
+template <int N, Scales kScales, bool kInt>
 void launch_join(const Epilogue &E, int64_t splits, hipStream_t stream) {
   const int64_t vectors = E.rows * ceil_div<int64_t>(E.cols, N);
   if (splits > 4)
-    hipLaunchKernelGGL((k_join<8, N, kScales>), dim3(unsigned(ceil_div<int64_t>(vectors, 32))),
-                       dim3(256), 0, stream, E, int32_t(splits));
+    hipLaunchKernelGGL((k_join<8, N, kScales, kInt>),
+                       dim3(unsigned(ceil_div<int64_t>(vectors, 32))), dim3(256), 0, stream, E,
+                       int32_t(splits));
   else
-    hipLaunchKernelGGL((k_join<1, N, kScales>), dim3(unsigned(ceil_div<int64_t>(vectors, 256))),
-                       dim3(256), 0, stream, E, int32_t(splits));
+    hipLaunchKernelGGL((k_join<1, N, kScales, kInt>),
+                       dim3(unsigned(ceil_div<int64_t>(vectors, 256))), dim3(256), 0, stream, E,
+                       int32_t(splits));
 }
+template <typename S>
 hipError_t join(const Epilogue &E, int64_t splits, hipStream_t stream) {
-  const bool wide = E.dtype == HG_DT_F32;
-  if (E.col_scale)
-    wide ? launch_join<4, Scales::kAny>(E, splits, stream)
-         : launch_join<8, Scales::kAny>(E, splits, stream);
-  else
-    wide ? launch_join<4, Scales::kNone>(E, splits, stream)
-         : launch_join<8, Scales::kNone>(E, splits, stream);
+  constexpr Scales kScales = kIs8<S> ? Scales::kAny : Scales::kNone;
+  E.dtype == HG_DT_F32 ? launch_join<4, kScales, kWhole<S>>(E, splits, stream)
+                       : launch_join<8, kScales, kWhole<S>>(E, splits, stream);
   return hipGetLastError();
 }
 
@@ -1309,7 +1303,7 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
       else
         launch_few<S, 2>(A, p, stream);
       const hipError_t e = hipGetLastError();
-      return e != hipSuccess || p.splits == 1 ? e : join(A.E, p.splits, stream);
+      return e != hipSuccess || p.splits == 1 ? e : join<S>(A.E, p.splits, stream);
     }
   }
   if (E.cols > kMostCols) {
@@ -1348,7 +1342,7 @@ hipError_t product(Operand P, Operand Q, int64_t depth, Epilogue E, float *parts
     else
       launch_direct<S, TP, TQ, 256, 256, 2, 4, 128, 2>(B, grid, stream);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.splits > 1) e = join(B.E, p.splits, stream);
+    if (e == hipSuccess && p.splits > 1) e = join<S>(B.E, p.splits, stream);
     if (e != hipSuccess) return e;
     done += p.rows;
   }

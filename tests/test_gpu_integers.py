@@ -153,3 +153,30 @@ def test_repeats_streams_and_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+# depths that are cut (few rows; 64 x 64 and 128 x 128 tiles, by LDS and through registers; many parts)
+CUT = [(1, 8192, 1024), (9, 8192, 40), (32, 4096, 100), (64, 8192, 1024), (300, 65_536, 64),
+       (130, 20_000, 144), (400, 30_001, 260), (300, 8192, 1024), (2, 131_071, 33)]
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("m,k,n", CUT)
+def test_parts_that_cancel(m, k, n, out):
+    """Parts far past 2^24 that cancel: the sum is exact before it is rounded, however the depth is cut."""
+    x, w = ints(m, k, seed=1, lo=64), ints(n, k, seed=2, lo=64)
+    w[:, k // 2:] *= -1
+    one = torch.ones(max(m, n), device="cuda")
+    y = hg.linear(x, w, x_scale=one[:m], w_scale=one[:n], out_dtype=out)[0]
+    # (whole numbers below 2^53; to float32 and then to the result's type, as the header has it)
+    assert torch.equal(y, (x.double() @ w.double().t()).float().to(out))
+
+
+def test_a_row_is_the_same_among_others():
+    k, n = 8192, 1024
+    x, w, xs, ws = ints(2100, k, seed=1, lo=64), ints(n, k, seed=2, lo=64), scales(2100), scales(n)
+    w[:, k // 2:] *= -1
+    first = hg.linear(x[:1], w, x_scale=xs[:1], w_scale=ws, out_dtype=F32)[0]
+    for m in (2, 20, 33, 64, 300, 2100):
+        y = hg.linear(x[:m], w, x_scale=xs[:m], w_scale=ws, out_dtype=F32)[0]
+        assert torch.equal(y[:1], first), m
