@@ -82,16 +82,6 @@ __device__ __forceinline__ void integers(const float *x, float c, float f, bool 
   for (int k = 0; k < N / 4; ++k)
     w[k] = broken ? 0 : pack_i8(q[4 * k], q[4 * k + 1], q[4 * k + 2], q[4 * k + 3]);
 }
-template <int N>
-__device__ __forceinline__ void store_words(uint8_t *p, const uint32_t *w, int n) {
-  if (n >= N) {
-    __builtin_memcpy(p, w, N);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < n) p[i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
-  }
-}
 
 // G lanes take a group of columns: `groups` of `width` columns a row.  NV times kWide neighbours a
 // lane hold it; walks over the groups, the next one's loads in flight while this one is written.

@@ -79,19 +79,25 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
 }
 
+// N bytes of words, n (>= 1) of them in memory.
+template <int N>
+__device__ __forceinline__ void store_words(uint8_t *p, const uint32_t *w, int n) {
+  if (n >= N) {
+    __builtin_memcpy(p, w, N);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
+  }
+}
+
 template <int V>
 __device__ __forceinline__ void store_e4m3(uint8_t *p, const float *v, int n) {
   uint32_t w[V / 4];
 #pragma unroll
   for (int i = 0; i < V / 4; ++i)
     w[i] = pack_e4m3(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-  if (n >= V) {
-    __builtin_memcpy(p, w, V);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < n) p[i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
-  }
+  store_words<V>(p, w, n);
 }
 
 // Integers have neither NaN nor infinities: a row (or group) that has one is zeros with a
@@ -105,20 +111,6 @@ __device__ __forceinline__ uint32_t pack_i8(float a, float b, float c, float d) 
   const uint32_t ab = __builtin_amdgcn_perm(bits(b), bits(a), 0x0c0c0400u);
   const uint32_t cd = __builtin_amdgcn_perm(bits(d), bits(c), 0x04000c0cu);
   return ab | cd;
-}
-template <int V>
-__device__ __forceinline__ void store_i8(uint8_t *p, const float *v, int n) {
-  uint32_t w[V / 4];
-#pragma unroll
-  for (int i = 0; i < V / 4; ++i)
-    w[i] = pack_i8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-  if (n >= V) {
-    __builtin_memcpy(p, w, V);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < n) p[i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
-  }
 }
 
 // V values of a vector over the columns, in float32 or T (HG_DT_NONE: all `none`).

@@ -332,3 +332,23 @@ def test_squares_past_the_range(dtype, dim):
         want = hg.layer_norm_grad(dy[good], x[good], w, dsum=None if ds is None else ds[good])
         assert torch.isnan(dx[bad].float()).all() and torch.equal(dx[good], want[0])
         assert torch.isnan(dw).all() and torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("dim", [32, 250, 1000, 2048, 9000])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -95, 2.0 ** -112, 2.0 ** -119, 2.0 ** 120])
+def test_8_bits_are_the_quotients(dim, size):
+    """The integer (or e4m3 value) is that of y / scale as float32 rounds it: bit for bit what quantize
+    makes of the same rows.  (53 bits round to 24 as the quotient itself does: 53 >= 2 x 24 + 2.)"""
+    rows = (1 << 21) // dim
+    x = rand(rows, dim, seed=dim, shift=0.3)
+    w, b = (1 + rand(dim, seed=1, scale=0.2)) * size, rand(dim, seed=2, scale=0.3) * size
+    y = hg.layer_norm(x, w, b)[0]
+    q, _, c = hg.layer_norm(x, w, b, out_dtype=I8)
+    want, wc = hg.quantize(y)
+    assert torch.equal(c, wc)
+    assert torch.equal(q, want), f"{int((q != want).sum())} of {q.numel()} integers"
+    q, _, c = hg.layer_norm(x, w, b, out_dtype=E4M3)
+    assert torch.equal(c, (y.abs().amax(1).double() / 448).float().clamp(min=2.0 ** -126))
+    want = (y.double() / c.double()[:, None]).float().to(E4M3)
+    off = q.view(torch.uint8) != want.view(torch.uint8)
+    assert not off.any(), f"{int(off.sum())} of {q.numel()} values"
