@@ -228,8 +228,8 @@ def linear(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=None,
 
 
 def linear_grad(dy, x, w, pre=None, act=None, want_dx: bool = True, want_dw: bool = True,
-                want_dbias: bool = True, dw_dtype=None, x_scale=None, pre_scale=None,
-                group: int = 0, stream=None):
+                want_dbias: bool = True, dw_dtype=None, stream=None, x_scale=None, pre_scale=None,
+                group: int = 0):
     """(dx, dw, dbias) of linear (hg_linear_grad).  pre: the forward call's, needed with an
     activation.  dw is in dw_dtype (default w's, or float32), dbias in float32.  The gradient
     of residual is dy.  What is not wanted is None.

@@ -2,6 +2,7 @@
 host, before any device work, and the binding refuses unfit tensors (no GPU needed; the pointers are
 never read)."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -152,3 +153,11 @@ def test_tensors_that_do_not_fit():
                  lambda: hg.dequantize(x.to(torch.int8), x[0])):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_stream_by_position():
+    """linear_grad's tenth argument is the stream, as it was before rows could be kept."""
+    t = torch.zeros(2, 2)
+    stream = types.SimpleNamespace(device=torch.device("cuda", 0))
+    with pytest.raises(ValueError, match="a stream of cuda:0"):
+        hg.linear_grad(t, t, t, None, None, True, True, True, None, stream)
