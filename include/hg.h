@@ -746,7 +746,8 @@ hg_status hg_embed(const hg_embed_args *args, hipStream_t stream);
  * is accumulated, or with scale = -rate a step of descent in place; the other rows are left as they
  * are).  Without add every row is written, zeros where no id names it.  Ids outside [0, nodes) count
  * for nothing.  The sums are made in a fixed order, in float32, then scaled; an id may come any
- * number of times.  n below 2^31. */
+ * number of times.  n below 2^31.  dy's rows may stand beside dtable's in one array, but share no
+ * memory with them (HG_EINVAL). */
 typedef struct hg_embed_grad_args {
   int64_t n, nodes, dim;
   int32_t dtype;              /* of dy */

@@ -1,8 +1,10 @@
 // C entry points of the dense operators (include/hg.h): argument checks on the
 // host, then the launchers.  Nothing here allocates device memory or waits.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <numeric>
 
 #include "hg_dense.hpp"
 
@@ -39,6 +41,31 @@ Kept kept(const void *q, int64_t stride, const float *scale, int32_t group, int6
   k.scale = scale;
   k.groups = group ? ceil_div<int64_t>(cols, group) : 1;
   return k;
+}
+
+// A matrix in memory: rows of `width` bytes, `step` bytes apart (0: one row, or one for all).
+struct Span {
+  uintptr_t at;
+  int64_t rows, step, width;
+};
+Span span(const void *p, int64_t rows, int64_t stride, int64_t cols, int32_t dtype) {
+  const int64_t size = size_of(dtype);
+  // (a stride that no array has stays one)
+  const int64_t step = rows > 1 ? std::min(stride, int64_t(1) << 58) * size : 0;
+  return Span{reinterpret_cast<uintptr_t>(p), rows, step, cols * size};
+}
+// Whether two of them share memory: their extents meet, and so do the rows' places modulo the largest
+// step that both steps are multiples of.  (Rows that would miss each other by their number alone count
+// as sharing.)
+bool share(const Span &a, const Span &b) {
+  const auto end = [](const Span &s) {
+    return __int128(s.at) + __int128(s.rows - 1) * s.step + s.width;
+  };
+  if (a.at >= end(b) || b.at >= end(a)) return false;
+  const int64_t step = std::gcd(a.step, b.step);
+  if (step == 0) return true;
+  const int64_t off = int64_t(((__int128(b.at) - __int128(a.at)) % step + step) % step);
+  return off < a.width || off + b.width > step;
 }
 
 #define HG_REQUIRE(cond, ...) \
@@ -219,6 +246,9 @@ hg_status hg_embed_grad(const hg_embed_grad_args *a, hipStream_t stream) {
     HG_REQUIRE(a->workspace && a->workspace_bytes >=
                                    hg_embed_grad_workspace(a->n, a->nodes, a->dim),
                "hg_embed_grad: workspace too small");
+    HG_REQUIRE(!share(span(a->dy, a->n, a->dy_stride, a->dim, a->dtype),
+                      span(a->dtable, a->nodes, a->dtable_stride, a->dim, a->out_dtype)),
+               "hg_embed_grad: dy and dtable share memory");
   }
   clear_pending();
   return launched(launch_embed_grad(*a, stream), "hg_embed_grad");

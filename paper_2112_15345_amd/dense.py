@@ -213,7 +213,7 @@ def embed_grad(dy, ids, nodes: int, scale: float = 1.0, out_dtype=None, into=Non
     scale times the sum of dy's rows over the positions of each id, in out_dtype (float32 by
     default, or dy's).  Ids out of range count for nothing.  into: a float32 table that it is
     added to in place, and that is returned; rows that no id names are not touched (with scale
-    = -rate a step of descent)."""
+    = -rate a step of descent).  dy shares no memory with it."""
     return _call("embed_grad", stream, dy, ids, nodes, scale, out_dtype, into)[0]
 
 

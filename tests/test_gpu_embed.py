@@ -239,3 +239,25 @@ def test_capture(n):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_table_and_rows_in_one_memory():
+    """dy may stand beside the table's rows, not in them (the rows would be read while others are written)."""
+    big = whole(60, 48, seed=1)
+    ids = some_ids(40, 60, "any", seed=1)
+    table = big[:, :16]
+    for dy in (table[:40], big[10:50, 8:24], big.view(120, 24)[::3, :16], table[3:4].expand(40, 16)):
+        kept = big.clone()
+        with pytest.raises(hg.HGError) as e:
+            hg.embed_grad(dy, ids[:len(dy)], 60, into=table)
+        assert e.value.status == hg.HG_EINVAL and torch.equal(big, kept)
+    for dy in (big[:40, 16:32], big[::2, 32:], big[5:6, 20:36].expand(40, 16), big[7:8, 16:32]):
+        m = len(dy)
+        want = table.double() + sums(dy.clone(), ids[:m], 60)
+        hg.embed_grad(dy, ids[:m], 60, into=table)
+        assert torch.equal(table.double(), want)
+    # above and below the table in one tensor
+    rows = whole(100, 16, seed=2)
+    want = rows[40:].double() + sums(rows[:40].clone(), ids, 60)
+    hg.embed_grad(rows[:40], ids, 60, into=rows[40:])
+    assert torch.equal(rows[40:].double(), want)

@@ -161,3 +161,16 @@ def test_stream_by_position():
     stream = types.SimpleNamespace(device=torch.device("cuda", 0))
     with pytest.raises(ValueError, match="a stream of cuda:0"):
         hg.linear_grad(t, t, t, None, None, True, True, True, None, stream)
+
+
+# (each is refused before any work on a device: dy's rows in the table's, or the table's in dy's)
+@pytest.mark.parametrize("kw", [
+    dict(), dict(add=1, dtype=1), dict(dtable=P + 16, dtable_stride=8), dict(dtable=P - 4 * 8 * 4),
+    dict(dtype=1, dy_stride=0, dtable=P - 60), dict(n=1, dy_stride=1 << 62),
+    dict(dtype=1, dy_stride=24, dtable_stride=16, dtable=P + 32),
+    dict(dtype=1, dy_stride=32, dtable_stride=16, dtable=P + 4 * 7),
+    dict(dtype=1, dy_stride=32, dtable_stride=16, dtable=P + 4 * 25 - 4 * 64),
+])
+def test_gradient_in_the_rows_that_it_is_made_of(kw):
+    assert embed_grad(**kw) == hg.HG_EINVAL
+    assert b"memory" in LIB.hg_last_error()
