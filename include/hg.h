@@ -879,7 +879,8 @@ int64_t hg_linear_grad_workspace(int64_t m, int64_t k, int64_t n, int32_t dtype,
  * slope there is 0); x's are rounded to `dtype` once. */
 typedef struct hg_linear_grad_kept_args {
   hg_linear_grad_args grad;   /* x and pre: int8 with strides in elements, where they are kept; the
-                                 workspace's size from hg_linear_grad_kept_workspace */
+                                 workspace's size from hg_linear_grad_kept_workspace, or, where x
+                                 is not kept or dw is NULL, hg_linear_grad_workspace's is enough */
   int32_t group;              /* 0 or HG_KEPT_GROUP */
   const float *x_scale;       /* [m] or [m, ceil(k / group)], or NULL: x is in dtype */
   const float *pre_scale;     /* [m] or [m, ceil(n / group)], or NULL: pre is in dtype */

@@ -369,10 +369,10 @@ hg_status hg_linear_grad_kept(const hg_linear_grad_kept_args *args, hipStream_t 
   Kept x, pre;
   if (args->x_scale) x = kept(a.x, a.x_stride, args->x_scale, args->group, a.k);
   if (args->pre_scale) pre = kept(a.pre, a.pre_stride, args->pre_scale, args->group, a.n);
-  return linear_grad(&a, x, pre, hg_linear_grad_kept_workspace(a.m, a.k, a.n, a.dtype, a.act),
-                     stream);
+  // (x is widened for dw alone)
+  const auto workspace = args->x_scale && a.dw ? hg_linear_grad_kept_workspace : hg_linear_grad_workspace;
+  return linear_grad(&a, x, pre, workspace(a.m, a.k, a.n, a.dtype, a.act), stream);
 }
-
 
 hg_status hg_distill(const hg_distill_args *a, hipStream_t stream) {
   HG_REQUIRE(a, "hg_distill: NULL arguments");

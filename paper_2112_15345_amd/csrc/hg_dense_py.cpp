@@ -664,8 +664,8 @@ PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const at::Tensor db = truth(args[7]) ? make({nn}, at::kFloat, dev) : at::Tensor();
     const bool kept = kept_x || kept_pre;
     const at::Tensor space =
-        workspace((kept ? api.linear_grad_kept_workspace : api.linear_grad_workspace)(
-                      m, k, nn, code_of(type), act),
+        workspace((kept_x && dw.defined() ? api.linear_grad_kept_workspace
+                                          : api.linear_grad_workspace)(m, k, nn, code_of(type), act),
                   dev);
     hg_linear_grad_kept_args all{};
     hg_linear_grad_args &a = all.grad;

@@ -1383,7 +1383,7 @@ hipError_t linear(const hg_linear_args &A, hipStream_t stream) {
 template <typename T>
 hipError_t linear_grad(const hg_linear_grad_args &A, const Kept &kept_x, const Kept &kept_pre,
                        hipStream_t stream) {
-  const GradSpace g = grad_space(A.m, A.k, A.n, A.dtype, A.act, kept_x.p != nullptr);
+  const GradSpace g = grad_space(A.m, A.k, A.n, A.dtype, A.act, kept_x.p && A.dw);
   char *const ws = static_cast<char *>(A.workspace);
   Operand dz{A.dy, A.dy_stride, A.m}, dz_turned{A.dy, A.dy_stride, A.n};
   const bool has_act = A.act != HG_ACT_NONE;
@@ -1439,7 +1439,8 @@ hipError_t linear_grad(const hg_linear_grad_args &A, const Kept &kept_x, const K
     hipError_t e = hipSuccess;
     if (kept_x.p && A.m > 0 && A.k > 0) {
       // what the rows stand for, in T (the products' instructions take it): a rounding more than
-      // the integers and their scales have, of 2^-9 at most where their own step is some 2^-8
+      // the integers and their scales have, of 2^-8 of each value at most (bfloat16; 2^-11 in float16)
+      // where half their own step is 2^-8 of the largest value that shares the scale
       const int64_t stride = padded(A.k, sizeof(T));
       e = launch_dequantize(kept_x, A.m, A.k, stride, A.dtype, ws + g.x, stride, true, stream);
       x = Operand{ws + g.x, stride, stride, true};

@@ -1,5 +1,6 @@
 """quantize, dequantize, and linear_grad from kept rows.  The integers are the definition's bit for bit:
 in float32, the quotients by division, on the CPU."""
+import ctypes
 import math
 
 import numpy as np
@@ -8,6 +9,7 @@ import torch
 
 import dense_ref as R
 import paper_2112_15345_amd as hg
+from paper_2112_15345_amd import dense
 from test_gpu_dense_linear import ACTS, rand
 
 pytestmark = pytest.mark.gpu
@@ -275,3 +277,55 @@ def test_backward_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_workspace_is_what_the_call_needs():
+    """Rows that stand for x are made where x is kept and dw is wanted, and nowhere else."""
+    m, k, n = 4096, 4096, 128
+    widened = m * k * 2
+    dy, w = rand(m, n, dtype=BF16, seed=1), rand(n, k, dtype=BF16, seed=2)
+    x, pre = rand(m, k, dtype=BF16, seed=3), rand(m, n, dtype=BF16, seed=4)
+    x8, xs = hg.quantize(x, group=GROUP)
+    pre8, ps = hg.quantize(pre, group=GROUP)
+
+    def taken(**kw):
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        got = hg.linear_grad(dy, pre=pre8, act="gelu", pre_scale=ps, group=GROUP, w=w, **kw)
+        peak = torch.cuda.max_memory_allocated() - before
+        return peak - sum(t.numel() * t.element_size() for t in got if t is not None)
+
+    both = taken(x=x8, x_scale=xs)
+    assert widened <= both
+    assert taken(x=x8, x_scale=xs, want_dw=False) <= both - widened
+    assert taken(x=x) <= both - widened
+
+
+def test_least_workspace_is_enough():
+    """By the C entry point: hg_linear_grad_workspace's size where x is not kept, or dw not wanted."""
+    m, k, n = 300, 250, 140
+    lib = hg.load_library()
+    dy, w = rand(m, n, dtype=BF16, seed=1), rand(n, k, dtype=BF16, seed=2)
+    x, pre = rand(m, k, dtype=BF16, seed=3), rand(m, n, dtype=BF16, seed=4)
+    x8, xs = hg.quantize(x)
+    pre8, ps = hg.quantize(pre)
+    need = lib.hg_linear_grad_workspace(m, k, n, 3, 2)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for kept in (True, False):
+        rows = x8 if kept else x
+        dx = torch.empty(m, k, dtype=BF16, device="cuda")
+        dw = None if kept else torch.empty(n, k, dtype=BF16, device="cuda")
+        db = torch.empty(n, device="cuda")
+        grad = dense.LinearGradArgs(
+            m=m, k=k, n=n, dtype=3, dw_dtype=3, act=2, dy=dy.data_ptr(), dy_stride=n,
+            pre=pre8.data_ptr(), pre_stride=n, x=rows.data_ptr(), x_stride=k, w=w.data_ptr(), w_stride=k,
+            dx=dx.data_ptr(), dx_stride=k, dw=None if kept else dw.data_ptr(), dw_stride=k,
+            dbias=db.data_ptr(), workspace=ws.data_ptr(), workspace_bytes=need)
+        args = dense.LinearGradKeptArgs(grad, 0, xs.data_ptr() if kept else None, ps.data_ptr())
+        stream = torch.cuda.current_stream().cuda_stream
+        assert lib.hg_linear_grad_kept(ctypes.byref(args), stream) == hg.HG_OK
+        want = hg.linear_grad(dy, rows, w, pre=pre8, act="gelu", x_scale=xs if kept else None,
+                              pre_scale=ps, want_dw=not kept)
+        assert torch.equal(dx, want[0]) and torch.equal(db, want[2])
+        assert kept or torch.equal(dw, want[1])
