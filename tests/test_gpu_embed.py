@@ -1,11 +1,14 @@
 """embed and embed_grad: types, odd sizes and strides, ids that repeat or count for nothing, every way
 the ids are sorted and the rows cut into chunks, adding in place, other streams, capture.  Sums of small
 whole numbers are exact in 32 bits, so that most gradients are compared bit for bit."""
+import ctypes
+
 import pytest
 import torch
 
 import dense_ref as R
 import paper_2112_15345_amd as hg
+from paper_2112_15345_amd import dense
 
 pytestmark = pytest.mark.gpu
 
@@ -239,6 +242,31 @@ def test_capture(n):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("n", [0, 100, 5000])
+@pytest.mark.parametrize("dtype,nodes,dim,gap", [(F32, 10_007, 5, 2), (BF16, 20_011, 7, 3),
+                                                 (F16, 3001, 9, 1), (F32, 9, 20_001, 5),
+                                                 (BF16, 5, 40_003, 11), (F32, 1, 33, 4)])
+def test_table_with_gaps(dtype, nodes, dim, gap, n):
+    """By the C entry point: a whole table's gradient into rows that do not follow each other.  Every row is
+    written, and nothing between them."""
+    lib = hg.load_library()
+    ids, dy = some_ids(n, nodes, "words", seed=1), whole(n, dim, dtype=dtype, seed=2)
+    code = {F32: 1, F16: 2, BF16: 3}[dtype]
+    for out, out_code in ((dtype, code), (F32, 1)):
+        buffer = torch.full((nodes, dim + gap), float("nan"), dtype=out, device="cuda")
+        ws = torch.empty(lib.hg_embed_grad_workspace(n, nodes, dim) + 16, dtype=torch.uint8,
+                         device="cuda")
+        args = dense.EmbedGradArgs(
+            n=n, nodes=nodes, dim=dim, dtype=code, out_dtype=out_code, scale=2.0, dy=dy.data_ptr(),
+            dy_stride=dim, ids=ids.data_ptr(), dtable=buffer.data_ptr(), dtable_stride=dim + gap,
+            workspace=ws.data_ptr(), workspace_bytes=ws.numel())
+        stream = torch.cuda.current_stream().cuda_stream
+        assert lib.hg_embed_grad(ctypes.byref(args), stream) == hg.HG_OK
+        # (sums of up to 5000 whole numbers up to 8: exact in 32 bits, rounded once)
+        assert torch.equal(buffer[:, :dim], (2 * sums(dy, ids, nodes)).float().to(out))
+        assert torch.isnan(buffer[:, dim:].float()).all()
 
 
 def test_table_and_rows_in_one_memory():
