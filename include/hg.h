@@ -664,7 +664,7 @@ int64_t hg_rms_norm_grad_workspace(int64_t rows, int64_t dim);
  *   out_dtype HG_DT_E4M3   scale_i = max(max_j |y_j| / 448, 2^-126),  y8_j = e4m3(y_j / scale_i)
  *   out_dtype HG_DT_I8     scale_i = max(max_j |y_j| (1 / 127), 2^-126),  y8_j = y_j / scale_i,
  *                          rounded to the nearest integer (of two as near, the even one)
- * (the quotients in float32: the integers are those that hg_quantize makes of y).
+ * (the quotients in float32: the integers are those that hg_quantize makes of y in float32).
  * The mean is taken first and the squares are summed around it, in float32.  A NaN or an infinity
  * anywhere in a row, or a sum (of h or of d_j^2, elements of some 1e19) past float32's range, makes
  * its y NaN (and its scale); in 8-bit integers, which have no NaN, the row is zeros and its scale

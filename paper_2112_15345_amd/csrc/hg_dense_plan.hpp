@@ -258,8 +258,9 @@ inline EmbedPlan embed_plan(int64_t n, int64_t nodes, int64_t dim) {
   p.digit = (p.bits + p.passes - 1) / p.passes;
   p.tiles = ceil_div<int64_t>(n, kSortTile);
   // chunks that fill the units, as long as they can be for that: each leaves up to two parts (us,
-  // 65537 words of 1024 columns by chunks of 16 / 32 / 64 / 128: 126 / 115 / 110 / 115; 175514 words
-  // of 25, 16 columns, by 8: 138, the parts' sums nearly all of it)
+  // 65537 words of 1024 columns by chunks of 16 / 32 / 64 / 128: 116 / 107 / 100 / 104; 175514 words
+  // of 25, 16 columns, by 8 / 32 / 64: 171 / 67 / 55, the parts' sums most of it; 20000 of 3000, 64
+  // columns, by 8 / 16 / 32 / 64: 42 / 41 / 46 / 57)
   p.chunk = 8;
   while (p.chunk < 64 && (n * std::min<int64_t>(dim, 2048) > (p.chunk << 21) || n > (p.chunk << 13)))
     p.chunk *= 2;

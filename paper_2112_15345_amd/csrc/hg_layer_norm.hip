@@ -19,7 +19,10 @@ namespace {
 // wavefront's / a block's: 1024 columns, 1 row 3.6 / 2.7, 512 4.2 / 3.5, 1024 4.4 / 4.4, 2048 5.2 /
 // 5.8, 8192 14.7 / 16.2; 2048 columns, 1 row 5.8 / 2.8, 1024 7.1 / 5.3, 8192 33.6 / 26.7; going
 // backward 1024 columns, 1 row 7.5 / 5.4, 512 9.3 / 8.0, 8192 24.6 / 27.9, 32768 59 / 80; 2048
-// columns, 1 row 11.6 / 5.6, 1024 14.5 / 12.3, 8192 59 / 37, 32768 134 / 102).
+// columns, 1 row 11.6 / 5.6, 1024 14.5 / 12.3, 8192 59 / 37, 32768 134 / 102; in float32, 512
+// columns, forward 1 row 3.3 / 2.7, 512 3.8 / 3.6, 1024 4.1 / 4.0, 2048 4.5 / 4.8, 32768 47 / 50, backward 1
+// row 6.2 / 5.1, 512 7.9 / 7.1, 1024 7.5 / 9.1, 8192 18 / 22; 300 columns, 512 rows 3.7 / 3.7 and 7.7 /
+// 7.2, 2048 4.4 / 5.5 and 8.8 / 10.6).
 constexpr int64_t kFewForward = 1024, kFewBackward = 512;
 template <typename F>
 hipError_t by_rows(int64_t rows, int64_t vecs, int64_t few, F f) {
@@ -103,7 +106,8 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm(hg_layer_norm_args A) {
   Group<G> grp(red);
   const int lane = threadIdx.x % G;
   const int dim = int(A.dim);
-  // (divided by, not multiplied with its reciprocal: the mean of equal elements is the element)
+  // (divided by, not multiplied with its reciprocal: the mean of equal elements whose sums are exact,
+  // as of up to 65536 in bfloat16, is the element)
   const float count = float(dim);
   const Source src{A.ids, A.x_rows};
   const int64_t step = int64_t(gridDim.x) * kRows;
@@ -297,7 +301,8 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_grad(hg_layer_norm_grad_a
   Group<G> grp(red);
   const int lane = threadIdx.x % G;
   const int dim = int(A.dim);
-  // (divided by, not multiplied with its reciprocal: the mean of equal elements is the element)
+  // (divided by, not multiplied with its reciprocal: the mean of equal elements whose sums are exact,
+  // as of up to 65536 in bfloat16, is the element)
   const float count = float(dim);
   const Source src{A.ids, A.x_rows};
   const int64_t step = int64_t(gridDim.x) * kRows;
@@ -427,7 +432,8 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_grad_long(hg_layer_norm_g
   __shared__ float red[Group<kBlock>::kLds];
   Group<kBlock> grp(red);
   const uint32_t dim = uint32_t(A.dim);
-  // (divided by, not multiplied with its reciprocal: the mean of equal elements is the element)
+  // (divided by, not multiplied with its reciprocal: the mean of equal elements whose sums are exact,
+  // as of up to 65536 in bfloat16, is the element)
   const float count = float(dim);
   const Source src{A.ids, A.x_rows};
   const Parts to(A);

@@ -33,7 +33,7 @@ struct F8 {
 // An element of 8-bit integers, whose products are summed exactly in 32-bit integers (of at most
 // 131071 terms of up to 2^14).  The sums stay in the registers (and the parts of a depth that is cut in
 // the places) of float32 ones until they are whole, and are rounded to float32 once.
-// 16384 x 4096 x 4096 with bias and residual: 258 us, 2.13e15 operations a second (2.6e15 at a depth of
+// 16384 x 4096 x 4096 with bias and residual: 261 us, 2.1e15 operations a second (2.6e15 at a depth of
 // 8192 without residual; the library's product of integers alone 281 us).
 struct I8 {
   int8_t b;
